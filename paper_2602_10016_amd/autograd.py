@@ -5,9 +5,12 @@ Marshalling only - every computation runs in the HIP library (see binding.py).
     gdpa(q, k, v, kv_offsets, scale, act, ...)                -> o    Eq. (GDPA) / softmax attention, jagged
     sliding_window_attention(q, k, v, offsets, left, right, scale, max_len)   -> o    Eq. (sliding window)
     sumkron_linear(x, z, w)                                   -> y    Eq. (SumKronLinear)
+    embedding(table, ids, scale)                              -> y    rows of a table by event id
+    layer_norm(x, weight, bias, eps)                          -> y    over the last axis
+    grouped_linear(x, w, offsets)                             -> y    one linear map per group of rows
 
-Inputs must be contiguous device tensors (bf16 or fp32); offsets are int32 device tensors and carry
-no gradient.  The incoming gradient is made contiguous before it is handed to the library.
+Inputs must be contiguous device tensors (bf16 or fp32); offsets (int32) and ids are device tensors
+and carry no gradient.  The incoming gradient is made contiguous before it is handed to the library.
 """
 import torch
 
@@ -76,3 +79,58 @@ class _SumKron(torch.autograd.Function):
 def sumkron_linear(x, z, w):
     """Y_b = sum_i Z_i^T X_b W_i;  x [B, S, D], z [k, S, T], w [k, D, D] -> y [B, T, D]."""
     return _SumKron.apply(x, z, w)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale):
+        ctx.save_for_backward(ids)
+        ctx.args = (table.shape[0], scale)
+        return kb.embedding_fwd(table, ids, scale)
+
+    @staticmethod
+    def backward(ctx, dy):
+        rows, scale = ctx.args
+        return kb.embedding_bwd(dy.contiguous(), ctx.saved_tensors[0], rows, scale), None, None
+
+
+def embedding(table, ids, scale=1.0):
+    """scale * table[ids];  table [rows, D], ids int32 or int64 of any shape (outside the table, as -1: zeros, no gradient)."""
+    return _Embedding.apply(table, ids, float(scale))
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = kb.layer_norm_fwd(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dx, dw, db = ctx.needs_input_grad[:3]
+        return *kb.layer_norm_bwd(x, weight, dy.contiguous(), mean, rstd, want_dx=dx, want_dw=dw, want_db=db), None
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Normalised over the last axis, times weight plus bias ([D] of x's dtype, or None)."""
+    return _LayerNorm.apply(x, weight, bias, float(eps))
+
+
+class _GroupedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, offsets):
+        ctx.save_for_backward(x, w, offsets)
+        return kb.grouped_linear_fwd(x, w, offsets)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w, offsets = ctx.saved_tensors
+        dx, dw = ctx.needs_input_grad[:2]
+        return *kb.grouped_linear_bwd(x, w, dy.contiguous(), offsets, want_dx=dx, want_dw=dw), None
+
+
+def grouped_linear(x, w, offsets):
+    """y[r] = x[r] @ w[g] for the rows offsets[g] .. offsets[g + 1] - 1;  x [total, K], w [G, K, N], offsets int32 [G + 1]."""
+    return _GroupedLinear.apply(x, w, offsets)

@@ -30,6 +30,10 @@ EXPORTS = ["kunlun_gdpa_fwd", "kunlun_gdpa_fwd_static", "kunlun_gdpa_bwd", "kunl
            "kunlun_sumkron_fwd", "kunlun_sumkron_workspace_bytes", "kunlun_sumkron_bwd", "kunlun_sumkron_bwd_workspace_bytes",
            "kunlun_check_offsets", "kunlun_stream_probe", "kunlun_jagged_stream_probe", "kunlun_strerror"]
 
+LAYER_EXPORTS = ["kunlun_embedding_fwd", "kunlun_embedding_bwd", "kunlun_embedding_bwd_workspace_bytes", "kunlun_layer_norm_fwd", "kunlun_layer_norm_bwd",
+                 "kunlun_layer_norm_bwd_workspace_bytes", "kunlun_grouped_linear_fwd", "kunlun_grouped_linear_bwd", "kunlun_grouped_linear_bwd_workspace_bytes"]
+MAX_CHANNELS, MAX_GROUPS = 16384, 4096
+
 _vp, _i, _i64, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 _lib.kunlun_gdpa_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i64, _i64, _f, _i, _vp, _i,
                                  _vp, _sz, _vp]
@@ -68,6 +72,24 @@ _lib.kunlun_stream_probe.argtypes = [_vp, _vp, _vp, _vp, _sz, _i, _i, _vp]
 _lib.kunlun_stream_probe.restype = _i
 _lib.kunlun_jagged_stream_probe.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i64, _i, _i, _i, _vp, _sz, _vp]
 _lib.kunlun_jagged_stream_probe.restype = _i
+_lib.kunlun_embedding_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _i, _f, _i, _i, _vp]
+_lib.kunlun_embedding_fwd.restype = _i
+_lib.kunlun_embedding_bwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _i, _f, _i, _i, _vp, _sz, _vp]
+_lib.kunlun_embedding_bwd.restype = _i
+_lib.kunlun_embedding_bwd_workspace_bytes.argtypes = [_i64, _i64, _i, _i]
+_lib.kunlun_embedding_bwd_workspace_bytes.restype = _sz
+_lib.kunlun_layer_norm_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i, _f, _i, _vp]
+_lib.kunlun_layer_norm_fwd.restype = _i
+_lib.kunlun_layer_norm_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i, _i, _vp, _sz, _vp]
+_lib.kunlun_layer_norm_bwd.restype = _i
+_lib.kunlun_layer_norm_bwd_workspace_bytes.argtypes = [_i64, _i, _i]
+_lib.kunlun_layer_norm_bwd_workspace_bytes.restype = _sz
+_lib.kunlun_grouped_linear_fwd.argtypes = [_vp, _vp, _vp, _vp, _i, _i64, _i, _i, _i, _i, _vp]
+_lib.kunlun_grouped_linear_fwd.restype = _i
+_lib.kunlun_grouped_linear_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i64, _i, _i, _i, _i, _vp, _sz, _vp]
+_lib.kunlun_grouped_linear_bwd.restype = _i
+_lib.kunlun_grouped_linear_bwd_workspace_bytes.argtypes = [_i, _i64, _i, _i, _i]
+_lib.kunlun_grouped_linear_bwd_workspace_bytes.restype = _sz
 _lib.kunlun_strerror.argtypes = [_i]
 _lib.kunlun_strerror.restype = ctypes.c_char_p
 
@@ -487,6 +509,214 @@ def sumkron_bwd(x, z, w, dy, *, workspace=None, stream=None):
     if rc != OK:
         raise KunlunError(rc)
     return dx, dz, dw
+
+
+# ---- the operators in front of attention (include/kunlun_layers.h) ----
+
+def _on_current_device(stream, **tensors):
+    """_on_device, and that the device is the current one and the stream's: the kernels are launched on the current device."""
+    _on_device(**tensors)
+    index = next(t.get_device() for t in tensors.values() if t is not None)
+    if index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
+    if isinstance(stream, torch.Stream) and stream.device.index != index:
+        raise ValueError(f"the tensors are on cuda:{index}, the stream is on {stream.device}")
+
+
+def _check_ids(ids):
+    if not isinstance(ids, torch.Tensor) or ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError("ids: expected an int32 or int64 tensor")
+    _check("ids", ids)
+
+
+def embedding_fwd(table, ids, scale=1.0, *, out=None, stream=None):
+    """kunlun_embedding_fwd.  table [rows, D], ids int32 or int64 of any shape; returns ids.shape + (D,): scale * table[ids], zeros for an
+    id outside the table (padding: -1)."""
+    done = _native.embedding_fwd(table, ids, scale, out, stream)
+    if done is not None:
+        return done
+    _check("table", table)
+    if table.dim() != 2:
+        raise ValueError(f"table: expected [rows, D], got shape {tuple(table.shape)}")
+    code = _dtype_code(table)
+    _check_ids(ids)
+    rows, D = table.shape
+    y = torch.empty((*ids.shape, D), dtype=table.dtype, device=table.device) if out is None else out
+    _check("out", y, like=table, shape=(*ids.shape, D))
+    _on_current_device(stream, table=table, ids=ids, out=y)
+    rc = _lib.kunlun_embedding_fwd(_ptr(table), _ptr(ids), _ptr(y), ids.numel(), rows, D, float(scale), ids.element_size(), code, _stream(stream))
+    if rc != OK:
+        raise KunlunError(rc)
+    return y
+
+
+def embedding_bwd_workspace_bytes(n, rows, D, dtype=BF16) -> int:
+    return int(_lib.kunlun_embedding_bwd_workspace_bytes(n, rows, D, dtype))
+
+
+def embedding_bwd(d_out, ids, rows, scale=1.0, *, out=None, workspace=None, stream=None):
+    """kunlun_embedding_bwd.  d_out ids.shape + (D,); returns the gradient of the table, [rows, D] (written into `out` when given)."""
+    done = _native.embedding_bwd(d_out, ids, rows, scale, out, workspace, stream)
+    if done is not None:
+        return done
+    _check_ids(ids)
+    _check("d_out", d_out)
+    code = _dtype_code(d_out)
+    if d_out.dim() != ids.dim() + 1:
+        raise ValueError(f"d_out: shape {tuple(d_out.shape)}, expected {(*ids.shape, 'D')}")
+    D, rows = d_out.shape[-1], int(rows)
+    _check("d_out", d_out, shape=(*ids.shape, D))
+    if rows < 0:
+        raise ValueError(f"rows: {rows}")
+    g = torch.empty((rows, D), dtype=d_out.dtype, device=d_out.device) if out is None else out
+    _check("out", g, like=d_out, shape=(rows, D))
+    ws = _workspace(workspace, embedding_bwd_workspace_bytes(ids.numel(), rows, D, code), d_out.device, stream)
+    _on_current_device(stream, d_out=d_out, ids=ids, out=g, workspace=ws)
+    rc = _lib.kunlun_embedding_bwd(_ptr(d_out), _ptr(ids), _ptr(g), ids.numel(), rows, D, float(scale), ids.element_size(), code, _ptr(ws), ws.numel(),
+                                   _stream(stream))
+    if rc != OK:
+        raise KunlunError(rc)
+    return g
+
+
+def _check_norm_rows(x):
+    _check("x", x)
+    if x.dim() < 1:
+        raise ValueError("x: expected [..., D]")
+    return x.shape[-1], x.numel() // max(x.shape[-1], 1), _dtype_code(x)
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, *, out=None, mean=None, rstd=None, want_stats=True, stream=None):
+    """kunlun_layer_norm_fwd over the last axis of x [..., D]; weight and bias [D] of x's dtype, or None.  Returns (y, mean, rstd), the
+    statistics float32 of shape x.shape[:-1] (None without want_stats unless they are given)."""
+    done = _native.layer_norm_fwd(x, weight, bias, eps, out, mean, rstd, want_stats, stream)
+    if done is not None:
+        return done
+    D, rows, code = _check_norm_rows(x)
+    _check("weight", weight, like=x, shape=(D,), optional=True)
+    _check("bias", bias, like=x, shape=(D,), optional=True)
+    y = torch.empty_like(x) if out is None else out
+    _check("out", y, like=x, shape=x.shape)
+    stats = x.shape[:-1]
+    if want_stats:
+        mean = torch.empty(stats, dtype=torch.float32, device=x.device) if mean is None else mean
+        rstd = torch.empty(stats, dtype=torch.float32, device=x.device) if rstd is None else rstd
+    _check("mean", mean, dtype=torch.float32, shape=stats, optional=True)
+    _check("rstd", rstd, dtype=torch.float32, shape=stats, optional=True)
+    _on_current_device(stream, x=x, weight=weight, bias=bias, out=y, mean=mean, rstd=rstd)
+    rc = _lib.kunlun_layer_norm_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), rows, D, float(eps), code, _stream(stream))
+    if rc != OK:
+        raise KunlunError(rc)
+    return y, mean, rstd
+
+
+def layer_norm_bwd_workspace_bytes(rows, D, dtype=BF16) -> int:
+    return int(_lib.kunlun_layer_norm_bwd_workspace_bytes(rows, D, dtype))
+
+
+def layer_norm_bwd(x, weight, dy, mean, rstd, *, want_dx=True, want_dw=None, want_db=None, out=None, workspace=None, stream=None):
+    """kunlun_layer_norm_bwd.  mean and rstd are results of layer_norm_fwd.  Returns (dx, dw, db), None for what is not wanted
+    (want_dw and want_db: by default as there is a weight); out: the three tensors to write, instead of the want_ arguments."""
+    done = _native.layer_norm_bwd(x, weight, dy, mean, rstd, want_dx, want_dw, want_db, out, workspace, stream)
+    if done is not None:
+        return done
+    D, rows, code = _check_norm_rows(x)
+    _check("weight", weight, like=x, shape=(D,), optional=True)
+    _check("dy", dy, like=x, shape=x.shape)
+    _check("mean", mean, dtype=torch.float32, shape=x.shape[:-1])
+    _check("rstd", rstd, dtype=torch.float32, shape=x.shape[:-1])
+    if out is None:
+        affine = weight is not None
+        dx = torch.empty_like(x) if want_dx else None
+        dw = x.new_empty(D) if (affine if want_dw is None else want_dw) else None
+        db = x.new_empty(D) if (affine if want_db is None else want_db) else None
+    else:
+        dx, dw, db = out
+        _check("out[0] (dx)", dx, like=x, shape=x.shape, optional=True)
+        _check("out[1] (dw)", dw, like=x, shape=(D,), optional=True)
+        _check("out[2] (db)", db, like=x, shape=(D,), optional=True)
+    ws = None
+    if workspace is not None or dw is not None or db is not None:
+        ws = _workspace(workspace, layer_norm_bwd_workspace_bytes(rows, D, code), x.device, stream)
+    _on_current_device(stream, x=x, weight=weight, dy=dy, mean=mean, rstd=rstd, dx=dx, dw=dw, db=db, workspace=ws)
+    rc = _lib.kunlun_layer_norm_bwd(_ptr(x), _ptr(weight), _ptr(dy), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dw), _ptr(db), rows, D, code, _ptr(ws),
+                                    0 if ws is None else ws.numel(), _stream(stream))
+    if rc != OK:
+        raise KunlunError(rc)
+    return dx, dw, db
+
+
+def _check_grouped(x, w, offsets):
+    _check("x", x)
+    code = _dtype_code(x)
+    if x.dim() != 2:
+        raise ValueError(f"x: expected [total, K], got shape {tuple(x.shape)}")
+    total, K = x.shape
+    _check("w", w, like=x)
+    if w.dim() != 3 or w.shape[1] != K:
+        raise ValueError(f"w: shape {tuple(w.shape)}, expected [G, {K}, N]")
+    G, _, N = w.shape
+    _check_offsets("offsets", offsets, G)
+    return total, K, G, N, code
+
+
+def _verify_groups(offsets, total, stream):
+    if VERIFY_OFFSETS:
+        if isinstance(stream, torch.Stream):
+            stream.synchronize()
+        last = int(offsets[-1].item())
+        if last > total:
+            raise ValueError(f"offsets: {last} rows, there are {total}")
+        _verify("offsets", offsets, last, total, stream)
+
+
+def grouped_linear_fwd(x, w, offsets, *, out=None, stream=None):
+    """kunlun_grouped_linear_fwd.  x [total, K], w [G, K, N], offsets int32 [G + 1]; returns y [total, N] with y[r] = x[r] @ w[g] for the rows
+    of group g.  Rows behind the last group are zero in a y that the call allocates and stay as they are in `out`."""
+    if not VERIFY_OFFSETS:
+        done = _native.grouped_linear_fwd(x, w, offsets, out, stream)
+        if done is not None:
+            return done
+    total, K, G, N, code = _check_grouped(x, w, offsets)
+    y = torch.empty((total, N), dtype=x.dtype, device=x.device) if out is None else out
+    _check("out", y, like=x, shape=(total, N))
+    _on_current_device(stream, x=x, w=w, offsets=offsets, out=y)
+    _verify_groups(offsets, total, stream)
+    rc = _lib.kunlun_grouped_linear_fwd(_ptr(x), _ptr(w), _ptr(y), _ptr(offsets), G, total, K, N, int(out is None), code, _stream(stream))
+    if rc != OK:
+        raise KunlunError(rc)
+    return y
+
+
+def grouped_linear_bwd_workspace_bytes(G, total, K, N, dtype=BF16) -> int:
+    return int(_lib.kunlun_grouped_linear_bwd_workspace_bytes(G, total, K, N, dtype))
+
+
+def grouped_linear_bwd(x, w, dy, offsets, *, want_dx=True, want_dw=True, out=None, workspace=None, stream=None):
+    """kunlun_grouped_linear_bwd.  Returns (dx, dw), None for what is not wanted; out: the two tensors to write, instead of the want_
+    arguments.  Rows of dx behind the last group: as in grouped_linear_fwd."""
+    if not VERIFY_OFFSETS:
+        done = _native.grouped_linear_bwd(x, w, dy, offsets, want_dx, want_dw, out, workspace, stream)
+        if done is not None:
+            return done
+    total, K, G, N, code = _check_grouped(x, w, offsets)
+    _check("dy", dy, like=x, shape=(total, N))
+    if out is None:
+        dx, dw = torch.empty_like(x) if want_dx else None, torch.empty_like(w) if want_dw else None
+    else:
+        dx, dw = out
+        _check("out[0] (dx)", dx, like=x, shape=x.shape, optional=True)
+        _check("out[1] (dw)", dw, like=x, shape=w.shape, optional=True)
+    ws = None
+    if workspace is not None or dw is not None:
+        ws = _workspace(workspace, grouped_linear_bwd_workspace_bytes(G, total, K, N, code), x.device, stream)
+    _on_current_device(stream, x=x, w=w, dy=dy, offsets=offsets, dx=dx, dw=dw, workspace=ws)
+    _verify_groups(offsets, total, stream)
+    rc = _lib.kunlun_grouped_linear_bwd(_ptr(x), _ptr(w), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(offsets), G, total, K, N, int(out is None), code,
+                                        _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream))
+    if rc != OK:
+        raise KunlunError(rc)
+    return dx, dw
 
 
 def stream_probe(a, b, c, out, reads, write, *, stream=None):

@@ -15,7 +15,18 @@
 #include <ATen/ATen.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 
-#include "../../include/kunlun.h"
+#include "../../include/kunlun_layers.h"
+
+// (weak: the module also loads in front of a library of the attention entry points alone)
+#pragma weak kunlun_embedding_fwd
+#pragma weak kunlun_embedding_bwd
+#pragma weak kunlun_embedding_bwd_workspace_bytes
+#pragma weak kunlun_layer_norm_fwd
+#pragma weak kunlun_layer_norm_bwd
+#pragma weak kunlun_layer_norm_bwd_workspace_bytes
+#pragma weak kunlun_grouped_linear_fwd
+#pragma weak kunlun_grouped_linear_bwd
+#pragma weak kunlun_grouped_linear_bwd_workspace_bytes
 
 // (of the library, behind its public interface: the bytes that one call of kunlun_sumkron_fwd can use)
 extern "C" size_t kunlun_sumkron_batch_bytes(int B, int S, int T, int D, int k, int dtype);
@@ -62,6 +73,47 @@ struct Call {
         if (s[1] > INT32_MAX || s[2] > INT32_MAX) return fail();
         if (t.scalar_type() != type || (a != ANY && s[0] != a) || (b != ANY && s[1] != b) || (c != ANY && s[2] != c)) return fail();
         return &t;
+    }
+    // A tensor of the call's dtype (the first one sets it) and any shape.
+    const at::Tensor* tensor(PyObject* o) {
+        if (!ok || !THPVariable_CheckExact(o)) return fail();
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!is_plain(t) || !same_device(t)) return fail();
+        if (type == at::ScalarType::Undefined) {
+            if (t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat) return fail();
+            type = t.scalar_type();
+        }
+        return t.scalar_type() == type ? &t : fail();
+    }
+    const at::Tensor* shaped(PyObject* o, at::IntArrayRef sizes) {
+        const at::Tensor* t = tensor(o);
+        return t && t->sizes() == sizes ? t : fail();
+    }
+    const at::Tensor* shaped_or_none(PyObject* o, at::IntArrayRef sizes) { return o == Py_None ? nullptr : shaped(o, sizes); }
+    // float32 statistics of rows
+    const at::Tensor* statistics(PyObject* o, at::IntArrayRef sizes) {
+        if (!ok || !THPVariable_CheckExact(o)) return fail();
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!is_plain(t) || t.scalar_type() != at::kFloat || t.sizes() != sizes || !same_device(t)) return fail();
+        return &t;
+    }
+    const at::Tensor* ids(PyObject* o) {
+        if (!ok || !THPVariable_CheckExact(o)) return fail();
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!is_plain(t) || (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) || !same_device(t)) return fail();
+        return &t;
+    }
+    // True or False (None: `otherwise`)
+    bool truth(PyObject* o, bool otherwise = false) {
+        if (o == Py_None) return otherwise;
+        if (o != Py_True && o != Py_False) ok = false;
+        return o == Py_True;
+    }
+    // The tensors' device is the current one and the stream's.
+    void on_current_device(PyObject* stream) {
+        if (!ok || c10::DeviceType::KUNLUN_CALL_DEVICE != c10::DeviceType::CUDA) return;
+        if (device != c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index()) ok = false;
+        if (stream != Py_None && THPStream_Check(stream) && ((THPStream*)stream)->device_index != device) ok = false;
     }
     // int32 offsets [n + 1] (n = ANY: any number of examples)
     const at::Tensor* offsets(PyObject* o, int64_t n) {
@@ -475,9 +527,192 @@ ENTRY(sumkron_bwd, 6)
     return grads.result();
 END_ENTRY
 
+// ---- the operators in front of attention (include/kunlun_layers.h) ----
+
+PyObject* wrapped_or_none(const Out& o, PyObject* given) { return o.t ? o.object(given) : Py_NewRef(Py_None); }
+
+// The outputs as a tuple; a given one is itself.
+template <size_t N>
+PyObject* tuple_of(const Out (&outs)[N], PyObject* const (&given)[N]) {
+    THPObjectPtr r(PyTuple_New(N));
+    if (!r) return nullptr;
+    for (size_t i = 0; i < N; ++i) {
+        PyObject* o = wrapped_or_none(outs[i], given[i]);
+        if (!o) return nullptr;
+        PyTuple_SET_ITEM(r.get(), i, o);
+    }
+    return r.release();
+}
+
+// `out` of a backward call: None, or a sequence of N tensors or Nones, which are held (as in Grads).
+template <size_t N>
+bool take_outs(Call& c, PyObject* out, THPObjectPtr (&held)[N]) {
+    if (out == Py_None) return false;
+    if (!(PyTuple_CheckExact(out) || PyList_CheckExact(out)) || PySequence_Fast_GET_SIZE(out) != (Py_ssize_t)N) { c.ok = false; return false; }
+    for (size_t i = 0; i < N; ++i) held[i] = Py_NewRef(PySequence_Fast_GET_ITEM(out, i));
+    return true;
+}
+
+// table, ids, scale, out, stream
+ENTRY(embedding_fwd, 5)
+    const at::Tensor* table = c.tensor(a[0]);
+    const at::Tensor* ids = c.ids(a[1]);
+    PLAIN_OR_NONE;
+    if (table->dim() != 2 || table->size(1) > INT32_MAX) Py_RETURN_NONE;
+    const int64_t rows = table->size(0), D = table->size(1);
+    std::vector<int64_t> sizes = ids->sizes().vec();
+    sizes.push_back(D);
+    const float scale = c.real(a[2]);
+    Out y;
+    if (a[3] != Py_None) y.t = c.shaped(a[3], sizes);
+    void* s = c.stream(a[4]);
+    c.on_current_device(a[4]);
+    PLAIN_OR_NONE;
+    if (!y.t) y.make(*table, sizes, table->scalar_type());
+    const int rc = enqueue(kunlun_embedding_fwd, table->data_ptr(), ids->data_ptr(), y.ptr(), ids->numel(), rows, (int)D, scale,
+                           (int)ids->element_size(), c.dtype(), s);
+    DONE_OR_NONE(rc);
+    return y.object(a[3]);
+END_ENTRY
+
+// d_out, ids, rows, scale, out, workspace, stream
+ENTRY(embedding_bwd, 7)
+    const at::Tensor* d_out = c.tensor(a[0]);
+    const at::Tensor* ids = c.ids(a[1]);
+    PLAIN_OR_NONE;
+    if (d_out->dim() != ids->dim() + 1 || d_out->sizes().slice(0, ids->dim()) != ids->sizes() || d_out->size(-1) > INT32_MAX) Py_RETURN_NONE;
+    const int64_t D = d_out->size(-1), n = ids->numel(), rows = c.integer(a[2]);
+    const float scale = c.real(a[3]);
+    if (rows < 0) Py_RETURN_NONE;
+    Out g, ws;
+    if (a[4] != Py_None) g.t = c.shaped(a[4], {rows, D});
+    take_workspace(c, a[5], ws);
+    void* s = c.stream(a[6]);
+    c.on_current_device(a[6]);
+    PLAIN_OR_NONE;
+    if (!g.t) g.make(*d_out, {rows, D}, d_out->scalar_type());
+    make_workspace(ws, *d_out, ws.t ? 0 : kunlun_embedding_bwd_workspace_bytes(n, rows, (int)D, c.dtype()), a[6]);
+    const int rc = enqueue(kunlun_embedding_bwd, d_out->data_ptr(), ids->data_ptr(), g.ptr(), n, rows, (int)D, scale,
+                           (int)ids->element_size(), c.dtype(), ws.ptr(), (size_t)ws.t->numel(), s);
+    DONE_OR_NONE(rc);
+    return g.object(a[4]);
+END_ENTRY
+
+// x, weight, bias, eps, out, mean, rstd, want_stats, stream
+ENTRY(layer_norm_fwd, 9)
+    const at::Tensor* x = c.tensor(a[0]);
+    PLAIN_OR_NONE;
+    if (x->dim() < 1 || x->size(-1) < 1 || x->size(-1) > INT32_MAX) Py_RETURN_NONE;
+    const int64_t D = x->size(-1);
+    const at::IntArrayRef per_row = x->sizes().slice(0, x->dim() - 1);
+    const at::Tensor* weight = c.shaped_or_none(a[1], {D});
+    const at::Tensor* bias = c.shaped_or_none(a[2], {D});
+    const float eps = c.real(a[3]);
+    Out o[3];
+    if (a[4] != Py_None) o[0].t = c.shaped(a[4], x->sizes());
+    for (int i = 1; i < 3; ++i)
+        if (a[4 + i] != Py_None) o[i].t = c.statistics(a[4 + i], per_row);
+    const bool want_stats = c.truth(a[7]);
+    void* s = c.stream(a[8]);
+    c.on_current_device(a[8]);
+    PLAIN_OR_NONE;
+    if (!o[0].t) o[0].make(*x, x->sizes(), x->scalar_type());
+    for (int i = 1; i < 3; ++i)
+        if (!o[i].t && want_stats) o[i].make(*x, per_row, at::kFloat);
+    const int rc = enqueue(kunlun_layer_norm_fwd, x->data_ptr(), data<void>(weight), data<void>(bias), o[0].ptr(), (float*)o[1].ptr(),
+                           (float*)o[2].ptr(), x->numel() / D, (int)D, eps, c.dtype(), s);
+    DONE_OR_NONE(rc);
+    return tuple_of(o, {a[4], a[5], a[6]});
+END_ENTRY
+
+// x, weight, dy, mean, rstd, want_dx, want_dw, want_db, out, workspace, stream
+ENTRY(layer_norm_bwd, 11)
+    const at::Tensor* x = c.tensor(a[0]);
+    PLAIN_OR_NONE;
+    if (x->dim() < 1 || x->size(-1) < 1 || x->size(-1) > INT32_MAX) Py_RETURN_NONE;
+    const int64_t D = x->size(-1), rows = x->numel() / D;
+    const at::IntArrayRef per_row = x->sizes().slice(0, x->dim() - 1);
+    const at::Tensor* weight = c.shaped_or_none(a[1], {D});
+    const at::Tensor* dy = c.shaped(a[2], x->sizes());
+    const at::Tensor* mean = c.statistics(a[3], per_row);
+    const at::Tensor* rstd = c.statistics(a[4], per_row);
+    const bool want[3] = {c.truth(a[5]), c.truth(a[6], weight), c.truth(a[7], weight)};
+    PLAIN_OR_NONE;
+    Out o[3], ws;
+    THPObjectPtr held[3];
+    const bool given = take_outs(c, a[8], held);
+    const at::IntArrayRef column(D);
+    const at::IntArrayRef sizes[3] = {x->sizes(), column, column};
+    for (int i = 0; given && i < 3; ++i) o[i].t = c.shaped_or_none(held[i], sizes[i]);
+    take_workspace(c, a[9], ws);
+    void* s = c.stream(a[10]);
+    c.on_current_device(a[10]);
+    PLAIN_OR_NONE;
+    for (int i = 0; !given && i < 3; ++i)
+        if (want[i]) o[i].make(*x, sizes[i], x->scalar_type());
+    if (o[1].t || o[2].t) make_workspace(ws, *x, ws.t ? 0 : kunlun_layer_norm_bwd_workspace_bytes(rows, (int)D, c.dtype()), a[10]);
+    const int rc = enqueue(kunlun_layer_norm_bwd, x->data_ptr(), data<void>(weight), dy->data_ptr(), data<float>(mean), data<float>(rstd),
+                           o[0].ptr(), o[1].ptr(), o[2].ptr(), rows, (int)D, c.dtype(), ws.ptr(), (size_t)(ws.t ? ws.t->numel() : 0), s);
+    DONE_OR_NONE(rc);
+    return tuple_of(o, {given ? held[0].get() : Py_None, given ? held[1].get() : Py_None, given ? held[2].get() : Py_None});
+END_ENTRY
+
+// x, w, offsets, out, stream
+ENTRY(grouped_linear_fwd, 5)
+    const at::Tensor* x = c.tensor(a[0]);
+    const at::Tensor* w = c.tensor(a[1]);
+    PLAIN_OR_NONE;
+    if (x->dim() != 2 || w->dim() != 3 || w->size(1) != x->size(1)) Py_RETURN_NONE;
+    const int64_t total = x->size(0), K = x->size(1), G = w->size(0), N = w->size(2);
+    const at::Tensor* off = c.offsets(a[2], G);
+    for (int64_t n : {G, K, N})
+        if (n > INT32_MAX) c.ok = false;
+    Out y;
+    if (a[3] != Py_None) y.t = c.shaped(a[3], {total, N});
+    void* s = c.stream(a[4]);
+    c.on_current_device(a[4]);
+    PLAIN_OR_NONE;
+    if (!y.t) y.make(*x, {total, N}, x->scalar_type());
+    const int rc = enqueue(kunlun_grouped_linear_fwd, x->data_ptr(), w->data_ptr(), y.ptr(), data<int32_t>(off), (int)G, total, (int)K, (int)N,
+                           (int)(a[3] == Py_None), c.dtype(), s);
+    DONE_OR_NONE(rc);
+    return y.object(a[3]);
+END_ENTRY
+
+// x, w, dy, offsets, want_dx, want_dw, out, workspace, stream
+ENTRY(grouped_linear_bwd, 9)
+    const at::Tensor* x = c.tensor(a[0]);
+    const at::Tensor* w = c.tensor(a[1]);
+    PLAIN_OR_NONE;
+    if (x->dim() != 2 || w->dim() != 3 || w->size(1) != x->size(1)) Py_RETURN_NONE;
+    const int64_t total = x->size(0), K = x->size(1), G = w->size(0), N = w->size(2);
+    const at::Tensor* dy = c.shaped(a[2], {total, N});
+    const at::Tensor* off = c.offsets(a[3], G);
+    for (int64_t n : {G, K, N})
+        if (n > INT32_MAX) c.ok = false;
+    const bool want[2] = {c.truth(a[4]), c.truth(a[5])};
+    Out o[2], ws;
+    THPObjectPtr held[2];
+    const bool given = take_outs(c, a[6], held);
+    const at::Tensor* const like[2] = {x, w};
+    for (int i = 0; given && i < 2; ++i) o[i].t = c.shaped_or_none(held[i], like[i]->sizes());
+    take_workspace(c, a[7], ws);
+    void* s = c.stream(a[8]);
+    c.on_current_device(a[8]);
+    PLAIN_OR_NONE;
+    for (int i = 0; !given && i < 2; ++i)
+        if (want[i]) o[i].make(*like[i], like[i]->sizes(), like[i]->scalar_type());
+    if (o[1].t) make_workspace(ws, *x, ws.t ? 0 : kunlun_grouped_linear_bwd_workspace_bytes((int)G, total, (int)K, (int)N, c.dtype()), a[8]);
+    const int rc = enqueue(kunlun_grouped_linear_bwd, x->data_ptr(), w->data_ptr(), dy->data_ptr(), o[0].ptr(), o[1].ptr(), data<int32_t>(off),
+                           (int)G, total, (int)K, (int)N, (int)!given, c.dtype(), ws.ptr(), (size_t)(ws.t ? ws.t->numel() : 0), s);
+    DONE_OR_NONE(rc);
+    return tuple_of(o, {given ? held[0].get() : Py_None, given ? held[1].get() : Py_None});
+END_ENTRY
+
 #define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(gdpa_fwd), METHOD(gdpa_bwd), METHOD(seed_attn_fwd), METHOD(seed_attn_bwd), METHOD(swa_fwd), METHOD(swa_bwd),
-                         METHOD(sumkron_fwd), METHOD(sumkron_bwd), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(sumkron_fwd), METHOD(sumkron_bwd), METHOD(embedding_fwd), METHOD(embedding_bwd), METHOD(layer_norm_fwd), METHOD(layer_norm_bwd),
+                         METHOD(grouped_linear_fwd), METHOD(grouped_linear_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
