@@ -135,3 +135,26 @@ def test_rows_and_weights_beyond_32_bit_offsets(kb):
     R.check("dx", dx, *ref[0], dtype)
     R.check("dw", dw[38:], *ref[1], dtype)
     assert not bool(dw[:38].any())
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("sizes,K,N", [([9000, 3, 0, 11_000, 700], 1000, 1032), ([20_000, 300], 264, 1000), ([70_000, 0, 513], 72, 520), ([33, 66_000], 256, 256),
+                                       ([5000] * 8 + [17] * 8, 136, 392)])
+def test_large(kb, sizes, K, N, dtype):
+    """Against torch in 64 bits: the bounds of layer_refs with the magnitudes of a row's and a column's norms (Cauchy-Schwarz)."""
+    n, rest = sum(sizes), 100
+    off = offsets_of(sizes)
+    x, w, dy = R.normal((n + rest, K), dtype, 1), R.normal((len(sizes), K, N), dtype, 2, K ** -0.5), R.normal((n + rest, N), dtype, 3)
+    x[n:], dy[n:] = float("nan"), float("nan")
+    (y, ry), (dx, rx), (dw, rw) = R.guarded((n + rest, N), dtype), R.guarded(x.shape, dtype), R.guarded(w.shape, dtype)
+    kb.grouped_linear_fwd(x, w, off, out=y)
+    kb.grouped_linear_bwd(x, w, dy, off, out=(dx, dw))
+    assert R.untouched(ry) and R.untouched(rx) and R.untouched(rw) and bool(y[n:].isnan().all()) and bool(dx[n:].isnan().all())
+    assert not kb.grouped_linear_fwd(x, w, off)[n:].any() and torch.equal(kb.grouped_linear_bwd(x, w, dy, off)[1], dw)
+    for g, (a, b) in enumerate(zip(off.tolist(), off.tolist()[1:])):
+        for got, left, right in ((y[a:b], x[a:b], w[g]), (dx[a:b], dy[a:b], w[g].t().contiguous()), (dw[g], x[a:b].t().contiguous(), dy[a:b])):
+            left, right = left.double(), right.double()
+            ref = left @ right
+            bound = (left.shape[1] + 1) * R.U * left.norm(dim=1, keepdim=True) * right.norm(dim=0)
+            limit = 1.01 * (bound + R.HALF_STEP[dtype] * (ref.abs() + bound)) + 1e-37
+            assert bool(((got.double() - ref).abs() <= limit).all()), g
