@@ -57,108 +57,258 @@ __global__ __launch_bounds__(THREADS) void embedding_fwd_kernel(const T* __restr
 }
 
 // ---- sorting ----
+//
+// A stable radix sort of (key, position) pairs, 8 bytes each.  A pass counts the digits of every range of pairs, scans the counts over the
+// ranges, and moves the pairs: a workgroup takes SORT_TILE pairs at a time, ranks them (lanes of a wave by ballots over the digit's bits, waves in
+// order), puts them in order in LDS and writes runs of equal digits, which a scattered store per pair would turn into a memory transaction
+// each.  Up to SORT_TILE pairs one workgroup makes all passes in LDS in one launch.
 
-constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64;
+constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64, SORT_KEYS = 8;  // pairs per lane and tile
+constexpr int SORT_TILE = SORT_THREADS * SORT_KEYS;
 constexpr int DIGIT_MOST = 10;  // bits of a digit: two passes up to a million table rows
 constexpr int BINS_MOST = 1 << DIGIT_MOST;
-constexpr int SORT_BLOCKS = 128;  // most ranges of one pass: every range reads the counts of all
+constexpr int64_t SORT_RANGES = 512;  // most ranges of a pass
+constexpr unsigned SCAN_RANGES = 64;  // from more on a launch of its own scans the counts
 
 // Where a pass reads: the ids themselves (first pass) or the pairs of the pass before.  An id outside the table sorts as
 // `rows`, behind every id of the table.
 template <typename ID>
-__device__ __forceinline__ uint32_t key_at(const ID* ids, const uint32_t* keys, int64_t i, uint32_t rows) {
-    if (keys) return keys[i];
+__device__ __forceinline__ uint2 pair_at(const ID* ids, const uint2* pairs, int64_t i, uint32_t rows) {
+    if (pairs) return pairs[i];
     const ID id = ids[i];
-    return in_table(id, rows) ? (uint32_t)id : rows;
+    return make_uint2(in_table(id, rows) ? (uint32_t)id : rows, (uint32_t)i);
 }
 
 template <typename ID>
-__global__ __launch_bounds__(SORT_THREADS) void digit_count_kernel(const ID* __restrict__ ids, const uint32_t* __restrict__ keys,
-                                                                   uint32_t* __restrict__ counts, int64_t n, int64_t per_block, uint32_t rows,
+__global__ __launch_bounds__(SORT_THREADS) void digit_count_kernel(const ID* __restrict__ ids, const uint2* __restrict__ pairs,
+                                                                   uint32_t* __restrict__ counts, int64_t n, int64_t per_range, uint32_t rows,
                                                                    int shift, int bits) {
     __shared__ uint32_t count[BINS_MOST];
     const int bins = 1 << bits;
     for (int d = threadIdx.x; d < bins; d += SORT_THREADS) count[d] = 0;
     __syncthreads();
-    const int64_t begin = blockIdx.x * per_block, end = begin + per_block < n ? begin + per_block : n;
-    for (int64_t i = begin + threadIdx.x; i < end; i += SORT_THREADS) atomicAdd(&count[(key_at(ids, keys, i, rows) >> shift) & (bins - 1)], 1u);
+    const int64_t begin = blockIdx.x * per_range, end = begin + per_range < n ? begin + per_range : n;
+    for (int64_t i0 = begin + threadIdx.x; i0 < end; i0 += SORT_TILE) {
+        uint32_t k[SORT_KEYS];
+#pragma unroll
+        for (int u = 0; u < SORT_KEYS; ++u) k[u] = pair_at(ids, pairs, i0 + u * SORT_THREADS < end ? i0 + u * SORT_THREADS : i0, rows).x;
+#pragma unroll
+        for (int u = 0; u < SORT_KEYS; ++u)
+            if (i0 + u * SORT_THREADS < end) atomicAdd(&count[(k[u] >> shift) & (bins - 1)], 1u);
+    }
     __syncthreads();
     for (int d = threadIdx.x; d < bins; d += SORT_THREADS) counts[(int64_t)blockIdx.x * bins + d] = count[d];
 }
 
-// Stable: ranges in order, waves in order inside a range, 64 pairs at a time inside a wave, lanes in order.
-template <typename ID>
-__global__ __launch_bounds__(SORT_THREADS) void digit_scatter_kernel(const ID* __restrict__ ids, const uint32_t* __restrict__ keys,
-                                                                     const uint32_t* __restrict__ positions, const uint32_t* __restrict__ counts,
-                                                                     uint32_t* __restrict__ keys_out, uint32_t* __restrict__ positions_out, int64_t n,
-                                                                     int64_t per_block, uint32_t rows, int shift, int bits) {
-    __shared__ uint32_t next[SORT_WAVES][BINS_MOST];  // where a wave's next pair of a digit goes
-    __shared__ uint32_t wave_sums[SORT_WAVES];
-    const int bins = 1 << bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t begin = blockIdx.x * per_block, end = begin + per_block < n ? begin + per_block : n;
-    const int64_t per_wave = per_block / SORT_WAVES;  // (a multiple of 64)
-    const int64_t w0 = begin + wave * per_wave, w1 = w0 + per_wave < end ? w0 + per_wave : end;
-    for (int d = lane; d < bins; d += 64) next[wave][d] = 0;
-    __syncthreads();
-    for (int64_t i = w0 + lane; i < w1; i += 64) atomicAdd(&next[wave][(key_at(ids, keys, i, rows) >> shift) & (bins - 1)], 1u);
-    // pairs of smaller digits in all ranges, and of this digit in the ranges before
-    uint32_t carry = 0;
-    for (int d0 = 0; d0 < bins; d0 += SORT_THREADS) {
-        const int d = d0 + threadIdx.x;
-        uint32_t all = 0, before = 0;
-        if (d < bins)
-            for (int b = 0; b < (int)gridDim.x; ++b) {
-                const uint32_t c = counts[(int64_t)b * bins + d];
-                all += c;
-                before += b < (int)blockIdx.x ? c : 0;
-            }
-        uint32_t upto = all;  // inclusive sum over the lanes, then over the waves
+// counts[range][digit] -> the sum over the ranges before; totals[digit].  32 digits x 32 parts of the ranges per workgroup.
+constexpr int SCAN_PARTS = 32, SCAN_FETCH = 16;  // loads in flight
+__global__ __launch_bounds__(32 * SCAN_PARTS) void digit_scan_kernel(uint32_t* __restrict__ counts, uint32_t* __restrict__ totals, int ranges,
+                                                                     int bins) {
+    __shared__ uint32_t sums[SCAN_PARTS][32];
+    const int col = threadIdx.x & 31, part = threadIdx.x >> 5, mine = blockIdx.x * 32 + col, d = mine < bins ? mine : 0;
+    const bool has = mine < bins;
+    const int per = (ranges + SCAN_PARTS - 1) / SCAN_PARTS, r0 = part * per, r1 = r0 + per < ranges ? r0 + per : ranges;
+    uint32_t sum = 0;
+    for (int r = r0; r < r1; r += SCAN_FETCH) {
+        uint32_t c[SCAN_FETCH];
 #pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const uint32_t v = __shfl_up(upto, o);
-            if (lane >= o) upto += v;
-        }
-        __syncthreads();  // the sums of the chunk before are read; the waves' counts are complete
-        if (lane == 63) wave_sums[wave] = upto;
-        __syncthreads();
-        uint32_t base = carry + upto - all + before, total = 0;
-        for (int w = 0; w < SORT_WAVES; ++w) {
-            if (w < wave) base += wave_sums[w];
-            total += wave_sums[w];
-        }
-        carry += total;
-        if (d < bins)
-            for (int w = 0; w < SORT_WAVES; ++w) {
-                const uint32_t c = next[w][d];
-                next[w][d] = base;
-                base += c;
+        for (int u = 0; u < SCAN_FETCH; ++u) c[u] = counts[(int64_t)(r + u < r1 ? r + u : r) * bins + d];
+#pragma unroll
+        for (int u = 0; u < SCAN_FETCH; ++u) sum += r + u < r1 ? c[u] : 0;
+    }
+    sums[part][col] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int q = 0; q < part; ++q) before += sums[q][col];
+    if (part == SCAN_PARTS - 1 && has) totals[d] = before + sum;
+    for (int r = r0; r < r1; r += SCAN_FETCH) {
+        uint32_t c[SCAN_FETCH];
+#pragma unroll
+        for (int u = 0; u < SCAN_FETCH; ++u) c[u] = counts[(int64_t)(r + u < r1 ? r + u : r) * bins + d];
+#pragma unroll
+        for (int u = 0; u < SCAN_FETCH; ++u)
+            if (r + u < r1 && has) {
+                counts[(int64_t)(r + u) * bins + d] = before;
+                before += c[u];
             }
     }
+}
+
+// Sums over the digits before, of a number per digit: x[v] of digit BINS_MOST / SORT_THREADS * threadIdx.x + v.
+constexpr int DIGITS = BINS_MOST / SORT_THREADS;  // per thread
+__device__ __forceinline__ void scan_digits(uint32_t (&x)[DIGITS], uint32_t* wave_sums) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int v = 0; v < DIGITS; ++v) mine += x[v];
+    uint32_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const uint32_t y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+    }
+    if (lane == 63) wave_sums[wave] = upto;
     __syncthreads();
-    for (int64_t i0 = w0; i0 < w1; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const bool ok = i < w1;
-        const uint32_t key = ok ? key_at(ids, keys, i, rows) : 0;
-        const uint32_t d = (key >> shift) & (bins - 1);
+    uint32_t at = upto - mine;
+    for (int w = 0; w < wave; ++w) at += wave_sums[w];
+#pragma unroll
+    for (int v = 0; v < DIGITS; ++v) {
+        const uint32_t c = x[v];
+        x[v] = at;
+        at += c;
+    }
+}
+
+// Puts the first `count` pairs of a tile (pair u of a lane is number (wave * SORT_KEYS + u) * 64 + lane) into `sorted` in the order of
+// their digits.  next: scratch; afterwards begin[d] is where digit d begins.
+struct SortSpaceLds {
+    uint32_t next[SORT_WAVES][BINS_MOST];  // where a wave's next pair of a digit goes
+    uint32_t begin[BINS_MOST];
+    uint32_t wave_sums[SORT_WAVES];
+    uint2 sorted[SORT_TILE];
+};
+__device__ __forceinline__ void sort_tile(SortSpaceLds& s, const uint2 (&pair)[SORT_KEYS], int count, int shift, int bits) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << bits) - 1;
+    for (int d = lane; d < BINS_MOST; d += 64) s.next[wave][d] = 0;
+    uint32_t rank[SORT_KEYS];  // among the wave's pairs of the digit
+#pragma unroll
+    for (int u = 0; u < SORT_KEYS; ++u) {
+        const bool ok = (wave * SORT_KEYS + u) * 64 + lane < count;
+        const uint32_t d = (pair[u].x >> shift) & mask;
         uint64_t same = __builtin_amdgcn_ballot_w64(ok);  // lanes of this digit
         for (int b = 0; b < bits; ++b) {
             const uint64_t set = __builtin_amdgcn_ballot_w64((d >> b) & 1);
             same &= (d >> b) & 1 ? set : ~set;
         }
         const int first = ok ? __ffsll((unsigned long long)same) - 1 : lane;
-        uint32_t to = 0;
-        if (ok && lane == first) to = atomicAdd(&next[wave][d], (uint32_t)__popcll(same));
-        to = __shfl(to, first) + __popcll(same & (((uint64_t)1 << lane) - 1));
-        if (ok) {
-            keys_out[to] = key;
-            positions_out[to] = positions ? positions[i] : (uint32_t)i;
+        uint32_t r = 0;
+        if (ok && lane == first) r = atomicAdd(&s.next[wave][d], (uint32_t)__popcll(same));
+        rank[u] = __shfl(r, first) + __popcll(same & (((uint64_t)1 << lane) - 1));
+    }
+    __syncthreads();
+    uint32_t at[DIGITS];
+#pragma unroll
+    for (int v = 0; v < DIGITS; ++v) {
+        const int d = DIGITS * threadIdx.x + v;
+        uint32_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < SORT_WAVES; ++w) {
+            const uint32_t c = s.next[w][d];
+            s.next[w][d] = sum;
+            sum += c;
         }
+        at[v] = sum;
+    }
+    scan_digits(at, s.wave_sums);
+#pragma unroll
+    for (int v = 0; v < DIGITS; ++v) s.begin[DIGITS * threadIdx.x + v] = at[v];
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < SORT_KEYS; ++u)
+        if ((wave * SORT_KEYS + u) * 64 + lane < count) {
+            const uint32_t d = (pair[u].x >> shift) & mask;
+            s.sorted[s.begin[d] + s.next[wave][d] + rank[u]] = pair[u];
+        }
+    __syncthreads();
+}
+
+template <typename ID>
+__device__ __forceinline__ void load_tile(uint2 (&pair)[SORT_KEYS], const ID* ids, const uint2* pairs, int64_t i0, int count, uint32_t rows) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int u = 0; u < SORT_KEYS; ++u) {
+        const int i = (wave * SORT_KEYS + u) * 64 + lane;
+        pair[u] = pair_at(ids, pairs, i0 + (i < count ? i : count - 1), rows);
+    }
+}
+
+template <typename ID>
+__global__ __launch_bounds__(SORT_THREADS) void digit_move_kernel(const ID* __restrict__ ids, const uint2* __restrict__ pairs,
+                                                                  const uint32_t* __restrict__ counts, const uint32_t* __restrict__ totals,
+                                                                  uint2* __restrict__ out, uint32_t* __restrict__ keys_out,
+                                                                  uint32_t* __restrict__ positions_out, int64_t n, int64_t per_range, uint32_t rows,
+                                                                  int shift, int bits) {
+    __shared__ SortSpaceLds s;
+    __shared__ uint32_t to[BINS_MOST];  // where the range's next pair of a digit goes
+    const int bins = 1 << bits;
+    uint32_t at[DIGITS] = {}, before[DIGITS] = {};
+    const int d0 = DIGITS * threadIdx.x;
+    static_assert(DIGITS == 2, "a thread's counts are one load");
+    if (d0 < bins) {
+        if (totals) {
+            const uint2 all = *(const uint2*)(totals + d0), mine = *(const uint2*)(counts + (int64_t)blockIdx.x * bins + d0);
+            at[0] = all.x; at[1] = all.y; before[0] = mine.x; before[1] = mine.y;
+        } else {
+            for (int r0 = 0; r0 < (int)gridDim.x; r0 += SCAN_FETCH) {
+                uint2 c[SCAN_FETCH];
+#pragma unroll
+                for (int u = 0; u < SCAN_FETCH; ++u) c[u] = *(const uint2*)(counts + (int64_t)(r0 + u < (int)gridDim.x ? r0 + u : r0) * bins + d0);
+#pragma unroll
+                for (int u = 0; u < SCAN_FETCH; ++u) {
+                    if (r0 + u < (int)gridDim.x) { at[0] += c[u].x; at[1] += c[u].y; }
+                    if (r0 + u < (int)blockIdx.x) { before[0] += c[u].x; before[1] += c[u].y; }
+                }
+            }
+        }
+    }
+    scan_digits(at, s.wave_sums);
+#pragma unroll
+    for (int v = 0; v < DIGITS; ++v) to[d0 + v] = at[v] + before[v];
+    const int64_t begin = blockIdx.x * per_range, end = begin + per_range < n ? begin + per_range : n;
+    for (int64_t i0 = begin; i0 < end; i0 += SORT_TILE) {
+        const int count = end - i0 < SORT_TILE ? (int)(end - i0) : SORT_TILE;
+        uint2 pair[SORT_KEYS];
+        load_tile(pair, ids, pairs, i0, count, rows);
+        __syncthreads();  // the tile before is written out
+        sort_tile(s, pair, count, shift, bits);
+        for (int i = threadIdx.x; i < count; i += SORT_THREADS) {
+            const uint2 p = s.sorted[i];
+            const uint32_t d = (p.x >> shift) & (bins - 1);
+            const uint32_t at = to[d] + i - s.begin[d];
+            if (out) out[at] = p;
+            else {
+                keys_out[at] = p.x;
+                positions_out[at] = p.y;
+            }
+        }
+        if (i0 + SORT_TILE >= end) break;
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < DIGITS; ++v) {
+            const int d = d0 + v;
+            if (d < bins) to[d] += (d + 1 < bins ? s.begin[d + 1] : count) - s.begin[d];
+        }
+    }
+}
+
+template <typename ID>
+__global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const ID* __restrict__ ids, uint32_t* __restrict__ keys_out,
+                                                                  uint32_t* __restrict__ positions_out, int n, uint32_t rows, int passes, int bits) {
+    __shared__ SortSpaceLds s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint2 pair[SORT_KEYS];
+    load_tile(pair, ids, (const uint2*)nullptr, 0, n, rows);
+    for (int p = 0; p < passes; ++p) {
+        sort_tile(s, pair, n, p * bits, bits);
+        if (p + 1 < passes) {
+#pragma unroll
+            for (int u = 0; u < SORT_KEYS; ++u) {
+                const int i = (wave * SORT_KEYS + u) * 64 + lane;
+                pair[u] = s.sorted[i < n ? i : n - 1];
+            }
+            __syncthreads();
+        }
+    }
+    for (int i = threadIdx.x; i < n; i += SORT_THREADS) {
+        keys_out[i] = s.sorted[i].x;
+        positions_out[i] = s.sorted[i].y;
     }
 }
 
 // ---- sums of the rows of equal ids ----
 
 constexpr int ADD_FETCH = 8;  // rows in flight per lane group
+constexpr int JOIN_FETCH = 8, JOIN_ALONE = 16;  // partial sums in flight; ranges of a run that one lane group adds
 constexpr int ZERO_ROWS = 64; // table rows that a workgroup searches for
 
 __device__ __forceinline__ int64_t first_at_least(const uint32_t* keys, int64_t lo, int64_t hi, uint32_t key) {
@@ -250,32 +400,88 @@ __global__ __launch_bounds__(THREADS) void embedding_add_kernel(const T* __restr
     finish(i1 < n && keys[i1] == key);
 }
 
-// Runs that cross ranges: the lane group of the range where one begins adds its partial sums in order.
+// acc += the partial sums in slot 0 of the ranges begin .. end - 1, in order
+template <int W>
+__device__ __forceinline__ void add_ranges(float (&acc)[W], const float* partial, int64_t begin, int64_t end, int pieces, int c) {
+    for (int64_t r = begin; r < end; r += JOIN_FETCH) {
+        float x[JOIN_FETCH][W];
+#pragma unroll
+        for (int u = 0; u < JOIN_FETCH; ++u)
+            __builtin_memcpy(x[u], __builtin_assume_aligned(partial + ((r + u < end ? r + u : begin) * 2 * pieces + c) * W, W % 4 ? 4 : 16), sizeof(x[u]));
+#pragma unroll
+        for (int u = 0; u < JOIN_FETCH; ++u)
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[j] += r + u < end ? x[u][j] : 0.f;
+    }
+}
+
+// Runs that cross ranges.  The lane group of the range where one begins adds its partial sums in order; a run over more than JOIN_ALONE
+// ranges is shared by the lane groups of the workgroup, each of which adds a part, and the parts are added in order.
 template <typename T, int W>
 __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t* __restrict__ keys, const float* __restrict__ partial,
                                                                  T* __restrict__ d_table, int64_t n, uint32_t rows, int D, float scale, int lanes,
                                                                  int64_t chunk) {
+    __shared__ int64_t last_of[THREADS];     // of the run that begins in a lane group's range: the last range it is in (0: none to add)
+    __shared__ uint32_t key_of[THREADS];
+    __shared__ float parts[THREADS * W];     // [groups][lanes][W]
     const int pieces = (D + W - 1) / W;
-    const int c = blockIdx.y * 64 + threadIdx.x % lanes;
-    const int64_t walker = (int64_t)blockIdx.x * (THREADS / lanes) + threadIdx.x / lanes;
-    const int64_t i0 = walker * chunk, i1 = i0 + chunk;
-    if (i1 >= n || c >= pieces) return;
-    const uint32_t key = keys[i1 - 1];
-    if (key >= rows || keys[i1] != key || (i0 > 0 && keys[i0 - 1] == key)) return;
-    const int64_t last = (first_at_least(keys, i1, n, key + 1) - 1) / chunk;  // the range that holds the run's last pair
-    float acc[W];
-    const float* p = partial + ((walker * 2 + 1) * pieces + c) * W;
-#pragma unroll
-    for (int j = 0; j < W; ++j) acc[j] = p[j];
-    for (int64_t r = walker + 1; r <= last; ++r) {
-        p = partial + ((r * 2) * pieces + c) * W;
-#pragma unroll
-        for (int j = 0; j < W; ++j) acc[j] += p[j];
+    const int lane = threadIdx.x % lanes, c = blockIdx.y * 64 + lane, group = threadIdx.x / lanes, groups = THREADS / lanes;
+    const bool has = c < pieces;
+    const int64_t walker0 = (int64_t)blockIdx.x * groups, walker = walker0 + group, i0 = walker * chunk, i1 = i0 + chunk;
+    int64_t last = 0;
+    uint32_t key = 0;
+    if (i1 < n) {
+        key = keys[i1 - 1];
+        if (key < rows && keys[i1] == key && !(i0 > 0 && keys[i0 - 1] == key)) {
+            // the range that holds the run's last pair; most runs end in the next one
+            last = i1 + chunk >= n || keys[i1 + chunk] != key ? walker + 1 : (first_at_least(keys, i1 + chunk, n, key + 1) - 1) / chunk;
+        }
     }
-    Piece<T, W> y;
+    auto finish = [&](const float (&acc)[W], uint32_t k) {
+        Piece<T, W> y;
 #pragma unroll
-    for (int j = 0; j < W; ++j) y.v[j] = from_float<T>(acc[j] * scale);
-    store_piece<T, W>(d_table + (int64_t)key * D + piece_start(c, D, W), y);
+        for (int j = 0; j < W; ++j) y.v[j] = from_float<T>(acc[j] * scale);
+        if (has) store_piece<T, W>(d_table + (int64_t)k * D + piece_start(c, D, W), y);
+    };
+    const int cc = has ? c : pieces - 1;
+    const bool together = last - walker > JOIN_ALONE;
+    if (last && !together) {
+        float acc[W];
+        const float* p = partial + ((walker * 2 + 1) * pieces + cc) * W;
+#pragma unroll
+        for (int j = 0; j < W; ++j) acc[j] = p[j];
+        add_ranges<W>(acc, partial, walker + 1, last + 1, pieces, cc);
+        finish(acc, key);
+    }
+    if (lane == 0) {
+        last_of[group] = together ? last : 0;
+        key_of[group] = key;
+    }
+    __syncthreads();
+    for (int w = 0; w < groups; ++w) {
+        const int64_t end = last_of[w] + 1;
+        if (end == 1) continue;
+        const int64_t first = walker0 + w + 1, per = (end - first + groups - 1) / groups, mine = first + group * per;
+        float acc[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) acc[j] = 0.f;
+        if (group == 0) {
+            const float* p = partial + (((walker0 + w) * 2 + 1) * pieces + cc) * W;
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[j] = p[j];
+        }
+        add_ranges<W>(acc, partial, mine, mine + per < end ? mine + per : end, pieces, cc);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < W; ++j) parts[threadIdx.x * W + j] = acc[j];
+        __syncthreads();
+        if (group == 0) {
+            for (int g = 1; g < groups; ++g)
+#pragma unroll
+                for (int j = 0; j < W; ++j) acc[j] += parts[(g * lanes + lane) * W + j];
+            finish(acc, key_of[w]);
+        }
+    }
 }
 
 template <typename T>
@@ -309,55 +515,64 @@ int64_t ranges_at_most(int64_t n) {
 }
 
 struct SortSpace {
-    uint32_t *keys[2], *positions[2], *counts;
+    uint2* pairs[2];
+    uint32_t *keys, *positions;  // in the end
+    uint32_t *counts, *totals;
     float* partial;
     size_t bytes;
     SortSpace(char* base, int64_t n, int D, int dtype) {
-        const size_t pairs = align_up((size_t)n * 4, 256);
         size_t at = 0;
-        auto take = [&](size_t b) { char* p = base + at; at += b; return p; };
-        for (int i = 0; i < 2; ++i) {
-            keys[i] = (uint32_t*)take(pairs);
-            positions[i] = (uint32_t*)take(pairs);
-        }
-        counts = (uint32_t*)take((size_t)SORT_BLOCKS * BINS_MOST * 4);
+        auto take = [&](size_t b) { char* p = base + at; at += align_up(b, 256); return p; };
+        for (int i = 0; i < 2; ++i) pairs[i] = (uint2*)take((size_t)n * 8);
+        keys = (uint32_t*)take((size_t)n * 4);
+        positions = (uint32_t*)take((size_t)n * 4);
+        const int64_t tiles = (n + SORT_TILE - 1) / SORT_TILE;
+        counts = (uint32_t*)take((size_t)(tiles < SORT_RANGES ? tiles : SORT_RANGES) * BINS_MOST * 4);
+        totals = (uint32_t*)take(BINS_MOST * 4);
         const int W = dtype == KUNLUN_FP32 ? piece_width<float>(D) : piece_width<bf16_t>(D);
-        partial = (float*)take(align_up((size_t)ranges_at_most(n) * 2 * pieces_per_row(D, W) * W * 4, 256));
+        partial = (float*)take((size_t)ranges_at_most(n) * 2 * pieces_per_row(D, W) * W * 4);
         bytes = at;
     }
 };
 
 template <typename ID>
-int sort_ids(const void* ids, const SortSpace& s, int64_t n, int64_t rows, hipStream_t stream) {
+void sort_ids(const void* ids, const SortSpace& s, int64_t n, int64_t rows, hipStream_t stream) {
     int bits = 1;
     while (rows >> bits) ++bits;  // keys are 0 .. rows
     const int passes = (bits + DIGIT_MOST - 1) / DIGIT_MOST, digit = (bits + passes - 1) / passes;
-    constexpr int64_t STEP = SORT_WAVES * 64;
-    int64_t per_block = (n + SORT_BLOCKS - 1) / SORT_BLOCKS;
-    per_block = (per_block + STEP - 1) / STEP * STEP;
-    const unsigned blocks = (unsigned)((n + per_block - 1) / per_block);
-    for (int p = 0; p < passes; ++p) {
-        const uint32_t* keys = p ? s.keys[(p + 1) & 1] : nullptr;
-        const uint32_t* positions = p ? s.positions[(p + 1) & 1] : nullptr;
-        hipLaunchKernelGGL(digit_count_kernel<ID>, dim3(blocks), dim3(SORT_THREADS), 0, stream, (const ID*)ids, keys, s.counts, n, per_block,
-                           (uint32_t)rows, p * digit, digit);
-        hipLaunchKernelGGL(digit_scatter_kernel<ID>, dim3(blocks), dim3(SORT_THREADS), 0, stream, (const ID*)ids, keys, positions, s.counts,
-                           s.keys[p & 1], s.positions[p & 1], n, per_block, (uint32_t)rows, p * digit, digit);
+    if (n <= SORT_TILE) {
+        hipLaunchKernelGGL(sort_small_kernel<ID>, dim3(1), dim3(SORT_THREADS), 0, stream, (const ID*)ids, s.keys, s.positions, (int)n, (uint32_t)rows, passes,
+                           digit);
+        return;
     }
-    return (passes - 1) & 1;
+    const int64_t tiles = (n + SORT_TILE - 1) / SORT_TILE, per_range = (tiles + SORT_RANGES - 1) / SORT_RANGES * SORT_TILE;
+    const unsigned ranges = (unsigned)((n + per_range - 1) / per_range);
+    const int bins = 1 << digit;
+    // few ranges: every range sums the counts itself (34 ranges: 8 us for two passes less than with the launch between)
+    uint32_t* const totals = ranges > SCAN_RANGES ? s.totals : nullptr;
+    for (int p = 0; p < passes; ++p) {
+        const uint2* from = p ? s.pairs[(p + 1) & 1] : nullptr;
+        hipLaunchKernelGGL(digit_count_kernel<ID>, dim3(ranges), dim3(SORT_THREADS), 0, stream, (const ID*)ids, from, s.counts, n, per_range,
+                           (uint32_t)rows, p * digit, digit);
+        if (totals)
+            hipLaunchKernelGGL(digit_scan_kernel, dim3((unsigned)((bins + 31) / 32)), dim3(32 * SCAN_PARTS), 0, stream, s.counts, totals, (int)ranges,
+                               bins);
+        hipLaunchKernelGGL(digit_move_kernel<ID>, dim3(ranges), dim3(SORT_THREADS), 0, stream, (const ID*)ids, from, s.counts, totals,
+                           p + 1 < passes ? s.pairs[p & 1] : nullptr, s.keys, s.positions, n, per_range, (uint32_t)rows, p * digit, digit);
+    }
 }
 
 template <typename T, int W>
-void embedding_bwd(const void* d_out, const SortSpace& s, int sorted, void* d_table, int64_t n, int64_t rows, int D, float scale, hipStream_t stream) {
+void embedding_bwd(const void* d_out, const SortSpace& s, void* d_table, int64_t n, int64_t rows, int D, float scale, hipStream_t stream) {
     const int pieces = pieces_per_row(D, W), lanes = lanes_per_row(pieces), groups = THREADS / lanes;
     const int64_t chunk = add_chunk(n), ranges = (n + chunk - 1) / chunk;
     const int64_t add_blocks = (ranges + groups - 1) / groups, zero_all = (rows + ZERO_ROWS - 1) / ZERO_ROWS;
     const int64_t zero_blocks = zero_all < GRID_MOST ? zero_all : GRID_MOST;
     const unsigned tiles = (unsigned)((pieces + 63) / 64);
     hipLaunchKernelGGL((embedding_add_kernel<T, W>), dim3((unsigned)(add_blocks + zero_blocks), tiles), dim3(THREADS), 0, stream, (const T*)d_out,
-                       s.keys[sorted], s.positions[sorted], (T*)d_table, s.partial, n, (uint32_t)rows, D, scale, lanes, chunk, add_blocks);
+                       s.keys, s.positions, (T*)d_table, s.partial, n, (uint32_t)rows, D, scale, lanes, chunk, add_blocks);
     if (ranges > 1)
-        hipLaunchKernelGGL((embedding_join_kernel<T, W>), dim3((unsigned)add_blocks, tiles), dim3(THREADS), 0, stream, s.keys[sorted], s.partial,
+        hipLaunchKernelGGL((embedding_join_kernel<T, W>), dim3((unsigned)add_blocks, tiles), dim3(THREADS), 0, stream, s.keys, s.partial,
                            (T*)d_table, n, (uint32_t)rows, D, scale, lanes, chunk);
 }
 
@@ -380,14 +595,16 @@ size_t embedding_bwd_workspace(int64_t n, int D, int dtype) { return SortSpace(n
 hipError_t launch_embedding_bwd(const void* d_out, const void* ids, void* d_table, int64_t n, int64_t rows, int D, float scale,
                                 int id_bytes, int dtype, void* workspace, hipStream_t stream) {
     const SortSpace s((char*)workspace, n, D, dtype);
-    int sorted = 0;
-    if (n > 0) sorted = id_bytes == 8 ? sort_ids<int64_t>(ids, s, n, rows, stream) : sort_ids<int32_t>(ids, s, n, rows, stream);
+    if (n > 0) {
+        if (id_bytes == 8) sort_ids<int64_t>(ids, s, n, rows, stream);
+        else sort_ids<int32_t>(ids, s, n, rows, stream);
+    }
     if (dtype == KUNLUN_FP32) {
-        if (piece_width<float>(D) == 4) embedding_bwd<float, 4>(d_out, s, sorted, d_table, n, rows, D, scale, stream);
-        else embedding_bwd<float, 1>(d_out, s, sorted, d_table, n, rows, D, scale, stream);
+        if (piece_width<float>(D) == 4) embedding_bwd<float, 4>(d_out, s, d_table, n, rows, D, scale, stream);
+        else embedding_bwd<float, 1>(d_out, s, d_table, n, rows, D, scale, stream);
     } else {
-        if (piece_width<bf16_t>(D) == 8) embedding_bwd<bf16_t, 8>(d_out, s, sorted, d_table, n, rows, D, scale, stream);
-        else embedding_bwd<bf16_t, 1>(d_out, s, sorted, d_table, n, rows, D, scale, stream);
+        if (piece_width<bf16_t>(D) == 8) embedding_bwd<bf16_t, 8>(d_out, s, d_table, n, rows, D, scale, stream);
+        else embedding_bwd<bf16_t, 1>(d_out, s, d_table, n, rows, D, scale, stream);
     }
     return hipGetLastError();
 }

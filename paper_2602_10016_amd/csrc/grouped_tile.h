@@ -1,4 +1,4 @@
-// The bf16 matrix-core product of the grouped linear maps: one BM x BN tile of C = A B per workgroup, fp32 sums.
+// The matrix-core product of the grouped linear maps: one BM x BN tile of C = A B per workgroup, bf16 or fp32 operands, fp32 sums.
 //
 // An operand lies in memory with the contraction along its rows ("row form": [rows, contraction]) or across them ("column form":
 // [contraction, columns]).  y = x w has A in row form and B in column form, dx = dy w^T both in row form, dw = x^T dy both in column
@@ -16,7 +16,8 @@
 
 namespace kunlun {
 
-constexpr int GL_STEP = 64;                      // contraction values per step
+constexpr int GL_STEP_BYTES = 128;
+template <typename T> constexpr int GL_STEP = GL_STEP_BYTES / sizeof(T);  // contraction values per step
 constexpr uint32_t GL_OUTSIDE = 0x80000000u;     // an offset outside every descriptor
 
 // What a workgroup reads: `base` is the tile's first row (row form) or its first column in the first contraction row (column form).
@@ -26,13 +27,13 @@ struct GroupedOperand {
     int valid;       // rows (row form) or columns (column form) that exist, from the tile's first one on
 };
 
-// DMA of one operand tile: EXTENT rows or columns of C, 64 contraction values.
-template <int EXTENT, int WAVES, bool COLUMNS>
+// DMA of one operand tile: EXTENT rows or columns of C, one step of contraction values.
+template <typename T, int EXTENT, int WAVES, bool COLUMNS>
 struct GroupedDma {
-    static constexpr int BYTES = EXTENT * GL_STEP * 2;
+    static constexpr int E = sizeof(T), STEP = GL_STEP<T>, BYTES = EXTENT * GL_STEP_BYTES;
     static constexpr int LOADS = BYTES / 1024 / WAVES;  // load instructions per wave and step
     static_assert(LOADS >= 1 && LOADS * 1024 * WAVES == BYTES, "a tile splits evenly over the waves");
-    static constexpr int ROW_BYTES = COLUMNS ? EXTENT * 2 : GL_STEP * 2, CHUNKS = ROW_BYTES / 16, ROWS = 1024 / ROW_BYTES;
+    static constexpr int ROW_BYTES = COLUMNS ? EXTENT * E : GL_STEP_BYTES, CHUNKS = ROW_BYTES / 16, ROWS = 1024 / ROW_BYTES;
     static_assert(ROW_BYTES <= 1024, "a load instruction fills whole rows");
     uint32_t voff[LOADS];
     const char* base;
@@ -41,7 +42,7 @@ struct GroupedDma {
 
     __device__ static __forceinline__ int swizzle(int row) {
         if (!COLUMNS) return (row >> 1) & 7;
-        return ROW_BYTES >= 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+        return E == 4 ? 0 : ROW_BYTES >= 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
     }
     __device__ __forceinline__ int row_of(int i) const { return (wave_ * LOADS + i) * ROWS + lane_ / CHUNKS; }
     __device__ __forceinline__ int chunk_of(int i) const { return (lane_ % CHUNKS) ^ swizzle(row_of(i)); }
@@ -55,83 +56,105 @@ struct GroupedDma {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             int row = row_of(i), chunk = chunk_of(i);
-            if (COLUMNS) chunk = chunk * 8 < o.valid ? chunk : o.valid / 8 - 1;
+            if (COLUMNS) chunk = chunk * (16 / E) < o.valid ? chunk : o.valid / (16 / E) - 1;
             else row = row < o.valid ? row : o.valid - 1;
             voff[i] = (uint32_t)row * ld + chunk * 16;
         }
     }
-    // Step k: contraction values 64 k .. + 63 of which `left` exist.
+    // Step k: contraction values STEP k .. of which `left` exist.
     __device__ __forceinline__ void issue(int64_t k, int left, uint32_t lds) const {
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + wave_ * (LOADS * 1024));
-        const char* const from = base + (COLUMNS ? k * GL_STEP * ld : k * (GL_STEP * 2));
-        const uint32_t bytes = COLUMNS ? (uint32_t)(left < GL_STEP ? left : GL_STEP) * ld : span;
+        const char* const from = base + (COLUMNS ? k * STEP * ld : k * GL_STEP_BYTES);
+        const uint32_t bytes = COLUMNS ? (uint32_t)(left < STEP ? left : STEP) * ld : span;
         u32x4 rsrc = make_rsrc_words(from, bytes);
 #pragma unroll
         for (int i = 0; i < 4; ++i) rsrc[i] = __builtin_amdgcn_readfirstlane(rsrc[i]);
-        if (COLUMNS || left >= GL_STEP) {
+        if (COLUMNS || left >= STEP) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) load_to_lds_b128(rsrc, voff[i], 0, dst + i * 1024);
         } else {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) load_to_lds_b128(rsrc, chunk_of(i) * 8 < left ? voff[i] : GL_OUTSIDE, 0, dst + i * 1024);
+            for (int i = 0; i < LOADS; ++i) load_to_lds_b128(rsrc, chunk_of(i) * (16 / E) < left ? voff[i] : GL_OUTSIDE, 0, dst + i * 1024);
         }
     }
 };
 
-// Fragments of an operand tile for a wave whose rows (columns) of C start at `first` (a multiple of 32).
-template <int EXTENT, bool COLUMNS>
+// Fragments of an operand tile for a wave whose rows (columns) of C start at `first` (a multiple of 32): 16 bytes of contraction values per
+// lane.
+template <typename T> struct GroupedFragOf { typedef bf16x8 type; };
+template <> struct GroupedFragOf<float> { typedef f32x4 type; };
+template <typename T, int EXTENT, bool COLUMNS>
 struct GroupedFrag {
-    static constexpr int ROW_BYTES = COLUMNS ? EXTENT * 2 : GL_STEP * 2;
+    typedef typename GroupedFragOf<T>::type Frag;
+    static constexpr int E = sizeof(T), ROW_BYTES = COLUMNS ? EXTENT * E : GL_STEP_BYTES;
     int at[2];
     __device__ __forceinline__ void init(int lane, int first) {
         const int g = lane >> 5;
-        if (COLUMNS) {
+        at[1] = 0;
+        if constexpr (COLUMNS && E == 2) {
             const int s16 = lane & 15, hi16 = (lane >> 4) & 1;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int row = 8 * g + 4 * half + (s16 >> 2), x = ROW_BYTES >= 256 ? row & 3 : (row >> 1) & 1;
-                at[half] = row * ROW_BYTES + ((first / 32) << 6 ^ x << 6) + (16 * hi16 + 4 * (s16 & 3)) * 2;
+                at[half] = row * ROW_BYTES + (((first / 32) ^ x) << 6) + (16 * hi16 + 4 * (s16 & 3)) * 2;
             }
+        } else if constexpr (COLUMNS) {
+            at[0] = 4 * g * ROW_BYTES + (first + (lane & 31)) * 4;
         } else {
             const int row = first + (lane & 31);
             at[0] = row * ROW_BYTES + ((g ^ ((row >> 1) & 7)) << 4);
-            at[1] = 0;
         }
     }
-    // Contraction values 16 c + 8 g .. + 7 of the lane's row (column) in block b of 32
-    __device__ __forceinline__ bf16x8 read(const char* tile, int b, int c) const {
-        if (COLUMNS) return tr_pair(tile + c * 16 * ROW_BYTES + (at[0] ^ (b << 6)), tile + c * 16 * ROW_BYTES + (at[1] ^ (b << 6)));
-        return *(const bf16x8*)(tile + b * 32 * ROW_BYTES + (at[0] ^ (c << 5)));
+    // Chunk 2 c + g of the step's contraction values, of the lane's row (column) in block b of 32
+    __device__ __forceinline__ Frag read(const char* tile, int b, int c) const {
+        if constexpr (COLUMNS && E == 2) {
+            const char* const rows = tile + c * 16 * ROW_BYTES;
+            return tr_pair(rows + (at[0] ^ (b << 6)), rows + (at[1] ^ (b << 6)));
+        } else if constexpr (COLUMNS) {
+            const char* const rows = tile + c * 8 * ROW_BYTES + at[0] + b * 128;
+            Frag f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) f[t] = *(const float*)(rows + t * ROW_BYTES);
+            return f;
+        } else {
+            return *(const Frag*)(tile + b * 32 * ROW_BYTES + (at[0] ^ (c << 5)));
+        }
     }
 };
+__device__ __forceinline__ f32x16 grouped_mfma(bf16x8 a, bf16x8 b, f32x16 c) { return mfma32(a, b, c); }
+__device__ __forceinline__ f32x16 grouped_mfma(f32x4 a, f32x4 b, f32x16 c) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
+    return c;
+}
 
 template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct GroupedShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int WAVES = WM * WN, THREADS = WAVES * 64;
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;  // 32 x 32 blocks of a wave
-    static constexpr int A_BYTES = BM * GL_STEP * 2, STAGE = A_BYTES + BN * GL_STEP * 2;
+    static constexpr int A_BYTES = BM * GL_STEP_BYTES, STAGE = A_BYTES + BN * GL_STEP_BYTES;
     static constexpr int OUT_ROW = NB * 32 * 4 + 16, OUT = WAVES * 32 * OUT_ROW;  // 32 rows of a wave at a time, padded, room for fp32
     static constexpr int LDS = STAGES * STAGE > OUT ? STAGES * STAGE : OUT;
 };
 
 // acc[nb][mb] += the tile's product over `length` contraction values.
-template <typename S, bool A_COLUMNS, bool B_COLUMNS>
+template <typename S, typename T, bool A_COLUMNS, bool B_COLUMNS>
 __device__ __forceinline__ void grouped_product(f32x16 (&acc)[S::NB][S::MB], char* lds, const GroupedOperand& a, const GroupedOperand& b, int length,
                                                 int lane, int wave) {
-    GroupedDma<S::BM, S::WAVES, A_COLUMNS> dma_a;
-    GroupedDma<S::BN, S::WAVES, B_COLUMNS> dma_b;
+    GroupedDma<T, S::BM, S::WAVES, A_COLUMNS> dma_a;
+    GroupedDma<T, S::BN, S::WAVES, B_COLUMNS> dma_b;
     dma_a.init(a, lane, wave);
     dma_b.init(b, lane, wave);
-    GroupedFrag<S::BM, A_COLUMNS> frag_a;
-    GroupedFrag<S::BN, B_COLUMNS> frag_b;
+    GroupedFrag<T, S::BM, A_COLUMNS> frag_a;
+    GroupedFrag<T, S::BN, B_COLUMNS> frag_b;
     frag_a.init(lane, wave / S::WN * (S::BM / S::WM));
     frag_b.init(lane, wave % S::WN * (S::BN / S::WN));
     constexpr int LOADS = decltype(dma_a)::LOADS + decltype(dma_b)::LOADS;
-    const int steps = (length + GL_STEP - 1) / GL_STEP;
+    const int steps = (length + GL_STEP<T> - 1) / GL_STEP<T>;
     const uint32_t lds0 = lds_address(lds);
     auto issue = [&](int k, int stage) {
-        const int left = length - k * GL_STEP;
+        const int left = length - k * GL_STEP<T>;
         dma_a.issue(k, left, lds0 + stage * S::STAGE);
         dma_b.issue(k, left, lds0 + stage * S::STAGE + S::A_BYTES);
     };
@@ -148,8 +171,8 @@ __device__ __forceinline__ void grouped_product(f32x16 (&acc)[S::NB][S::MB], cha
         const char* tb = ta + S::A_BYTES;
         stage = stage == S::STAGES - 1 ? 0 : stage + 1;
 #pragma unroll
-        for (int c = 0; c < GL_STEP / 16; ++c) {
-            bf16x8 fa[S::MB], fb[S::NB];
+        for (int c = 0; c < GL_STEP_BYTES / 32; ++c) {
+            typename GroupedFragOf<T>::type fa[S::MB], fb[S::NB];
 #pragma unroll
             for (int mb = 0; mb < S::MB; ++mb) fa[mb] = frag_a.read(ta, mb, c);
 #pragma unroll
@@ -157,7 +180,7 @@ __device__ __forceinline__ void grouped_product(f32x16 (&acc)[S::NB][S::MB], cha
 #pragma unroll
             for (int nb = 0; nb < S::NB; ++nb)
 #pragma unroll
-                for (int mb = 0; mb < S::MB; ++mb) acc[nb][mb] = mfma32(fb[nb], fa[mb], acc[nb][mb]);
+                for (int mb = 0; mb < S::MB; ++mb) acc[nb][mb] = grouped_mfma(fb[nb], fa[mb], acc[nb][mb]);
         }
     }
     __syncthreads();  // every wave is done with the ring: it stages the output next

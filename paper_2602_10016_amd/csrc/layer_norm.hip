@@ -185,23 +185,29 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const T* __restrict__
     }
 }
 
-// out[c] = sum of partial[p][c] over the p: 32 columns x 8 ranges of p per workgroup, ranges joined in order.  Columns 0 .. D - 1 go to
+// out[c] = sum of partial[p][c] over the p: 32 columns x 32 ranges of p per workgroup, ranges joined in order.  Columns 0 .. D - 1 go to
 // dw, the rest to db.
+constexpr int RANGES = 32, COLUMN_FETCH = 8;
 template <typename T>
-__global__ __launch_bounds__(THREADS) void norm_columns_kernel(const float* __restrict__ partial, T* __restrict__ dw, T* __restrict__ db, int parts,
-                                                               int D) {
-    __shared__ float sums[8][32];
+__global__ __launch_bounds__(32 * RANGES) void norm_columns_kernel(const float* __restrict__ partial, T* __restrict__ dw, T* __restrict__ db,
+                                                                   int parts, int D) {
+    __shared__ float sums[RANGES][32];
     const int col = threadIdx.x & 31, range = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + col;
-    const int per = (parts + 7) / 8, p0 = range * per, p1 = p0 + per < parts ? p0 + per : parts;
+    const int c = blockIdx.x * 32 + col, held = c < 2 * D ? c : 0;
+    const int per = (parts + RANGES - 1) / RANGES, p0 = range * per, p1 = p0 + per < parts ? p0 + per : parts;
     float t = 0.f;
-    if (c < 2 * D)
-        for (int p = p0; p < p1; ++p) t += partial[(int64_t)p * 2 * D + c];
+    for (int p = p0; p < p1; p += COLUMN_FETCH) {
+        float x[COLUMN_FETCH];
+#pragma unroll
+        for (int u = 0; u < COLUMN_FETCH; ++u) x[u] = partial[(int64_t)(p + u < p1 ? p + u : p0) * 2 * D + held];
+#pragma unroll
+        for (int u = 0; u < COLUMN_FETCH; ++u) t += p + u < p1 ? x[u] : 0.f;
+    }
     sums[range][col] = t;
     __syncthreads();
     if (range != 0 || c >= 2 * D) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) t += sums[i][col];
+    for (int i = 1; i < RANGES; ++i) t += sums[i][col];
     T* out = c < D ? dw : db;
     if (out) out[c < D ? c : c - D] = from_float<T>(t);
 }
@@ -301,9 +307,9 @@ hipError_t launch_layer_norm_bwd(const void* x, const void* weight, const void* 
     if (partial) {
         const dim3 grid((unsigned)((2 * D + 31) / 32));
         if (dtype == KUNLUN_FP32)
-            hipLaunchKernelGGL(norm_columns_kernel<float>, grid, dim3(THREADS), 0, stream, partial, (float*)dw, (float*)db, parts, D);
+            hipLaunchKernelGGL(norm_columns_kernel<float>, grid, dim3(32 * RANGES), 0, stream, partial, (float*)dw, (float*)db, parts, D);
         else
-            hipLaunchKernelGGL(norm_columns_kernel<bf16_t>, grid, dim3(THREADS), 0, stream, partial, (bf16_t*)dw, (bf16_t*)db, parts, D);
+            hipLaunchKernelGGL(norm_columns_kernel<bf16_t>, grid, dim3(32 * RANGES), 0, stream, partial, (bf16_t*)dw, (bf16_t*)db, parts, D);
     }
     return hipGetLastError();
 }
