@@ -2,6 +2,8 @@
 // Groups have any sizes, so the work is cut into output tiles and a workgroup finds its tile from the offsets: tiles of rows are
 // counted per group (a launch has room for the tiles of any division of the rows, those left over end at once).
 // The products run on the matrix cores (grouped_tile.h).
+#include <cmath>
+
 #include "grouped_tile.h"
 #include "layers.h"
 
@@ -47,62 +49,68 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t* offsets, int G, 
         const uint64_t beyond = __builtin_amdgcn_ballot_w64(upto > t);
         if (beyond) {
             const int at = __ffsll((unsigned long long)beyond) - 1;
-            const int n = __shfl(tiles, at), k = (int)(t - (__shfl(upto, at) - n));
+            const int n = __builtin_amdgcn_readlane(tiles, at), k = (int)(t - (__builtin_amdgcn_readlane(upto, at) - n));
             r.group = g0 + at;
-            r.row0 = __shfl((int)lo, at) + (int64_t)k * height;
-            const int left = (int)(__shfl(len, at) - (int64_t)k * height);
-            r.rows = left < height ? left : height;
-            if (SLOTS && n > 1) r.slot = slots + __shfl(shared, at) - n + k;
+            r.row0 = __builtin_amdgcn_readlane((int)lo, at) + (int64_t)k * height;
+            const int64_t left = __builtin_amdgcn_readlane(len, at) - (int64_t)k * height;
+            r.rows = left < height ? (int)left : height;
+            if (SLOTS && n > 1) r.slot = slots + __builtin_amdgcn_readlane(shared, at) - n + k;
             break;
         }
-        t -= __shfl(upto, 63);
-        if (SLOTS) slots += __shfl(shared, 63);
+        t -= __builtin_amdgcn_readlane(upto, 63);
+        if (SLOTS) slots += __builtin_amdgcn_readlane(shared, 63);
     }
-    r.group = __builtin_amdgcn_readfirstlane(r.group);
-    r.rows = __builtin_amdgcn_readfirstlane(r.rows);
-    r.slot = __builtin_amdgcn_readfirstlane(r.slot);
-    r.row0 = __builtin_amdgcn_readfirstlane((int)r.row0);
     return r;
+}
+// All tiles, with those behind the last group or without.
+__device__ __forceinline__ int64_t count_row_tiles(const int32_t* offsets, int G, int64_t total, int height, bool rest) {
+    int64_t n = 0;
+    for (int g0 = 0; g0 <= G; g0 += 64) {
+        const int g = g0 + (int)(threadIdx.x & 63);
+        int64_t lo;
+        int len;
+        const int tiles = tiles_of(offsets, G, total, height, g, lo, len);
+        n += __builtin_amdgcn_readlane(wave_prefix(g < G || rest ? tiles : 0), 63);
+    }
+    return n;
 }
 // Row tiles that a launch has room for: every group, and the rows behind them, may end inside a tile.
 int64_t row_tiles(int G, int64_t total, int height) { return (total + height - 1) / height + G + 1; }
 
-// Output tiles in blocks of up to SUPER_M x SUPER_N, a block on one XCD (workgroup i runs on XCD i % 8) at a time: its workgroups share rows of
-// one operand and columns of the other in that XCD's L2.  Blocks go round the XCDs, so that tiles left over at the end cost all the same.
-struct TileOrder {
-    int64_t m_tiles;
-    int n_tiles, super_m, super_n;
-};
-__host__ __device__ inline int64_t super_blocks(const TileOrder& o) {
-    return (o.m_tiles + o.super_m - 1) / o.super_m * ((o.n_tiles + o.super_n - 1) / o.super_n);
+// Which output tile a workgroup takes, of m_tiles x n_tiles that there are (m_tiles is known on the device only).  Workgroup i runs on XCD
+// i % 8, and each XCD has its own L2: it takes `unit` tiles in a row (what it computes at a time), the XCDs in turn, and what is left of
+// the last turn is split evenly.  Tiles are numbered in bands of `band` row tiles, column after column, so that those at work on an XCD
+// share rows of one operand and columns of the other.
+__device__ __forceinline__ bool tile_of(int64_t m_tiles, int n_tiles, int band, int unit, int64_t& mt, int& nt) {
+    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, xcd = id & 7, j = id >> 3;
+    const int64_t all = m_tiles * n_tiles, turns = all / (8 * unit), rest = all - turns * 8 * unit, per = (rest + 7) / 8;
+    int64_t at = j / unit < turns ? (j / unit * 8 + xcd) * unit + j % unit : turns * 8 * unit + xcd * per + (j - turns * unit);
+    if (j / unit >= turns && (j - turns * unit >= per || at >= all)) return false;
+    const int64_t b = at / ((int64_t)band * n_tiles), first = b * band;
+    const int in = (int)(at - first * n_tiles), height = m_tiles - first < band ? (int)(m_tiles - first) : band;
+    mt = first + in % height;
+    nt = in / height;
+    return true;
 }
-__device__ __forceinline__ bool tile_of(const TileOrder& o, int64_t& mt, int& nt) {
-    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, j = id >> 3;
-    const int size = o.super_m * o.super_n, in = (int)(j % size), across = (o.n_tiles + o.super_n - 1) / o.super_n;
-    const int64_t block = j / size * 8 + (id & 7);
-    mt = block / across * o.super_m + in % o.super_m;
-    nt = (int)(block % across) * o.super_n + in / o.super_m;
-    return mt < o.m_tiles && nt < o.n_tiles;
-}
-// (two dimensions: one holds at most 2^32 threads)
-dim3 tile_grid(const TileOrder& o, int threads) {
-    const int64_t all = (super_blocks(o) + 7) / 8 * 8 * o.super_m * o.super_n, most = largest_grid(threads) / 8 * 8;
+// Room for `all` tiles (two dimensions: one holds at most 2^32 threads)
+dim3 tile_grid(int64_t all, int threads) {
+    all = (all + 7) / 8 * 8;
+    const int64_t most = largest_grid(threads) / 8 * 8;
     return all <= most ? dim3((unsigned)all) : dim3((unsigned)most, (unsigned)((all + most - 1) / most));
 }
 
 // out[r, :] = in[r, :] W  (B_COLUMNS: W = w[g] [K, N];  else W = w[g]^T of w[g] [N, K])
 template <typename S, typename T, bool B_COLUMNS>
-__global__ __launch_bounds__(S::THREADS) void grouped_rows_kernel(const T* __restrict__ in, const T* __restrict__ w, T* __restrict__ out,
+__global__ __launch_bounds__(S::THREADS, 2) void grouped_rows_kernel(const T* __restrict__ in, const T* __restrict__ w, T* __restrict__ out,
                                                                   const int32_t* __restrict__ offsets, int G, int64_t total, int K, int N,
-                                                                  bool fill_rest, TileOrder order) {
+                                                                  bool fill_rest, int n_tiles, int band) {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t mt;
     int nt;
-    if (!tile_of(order, mt, nt)) return;
+    if (!tile_of(count_row_tiles(offsets, G, total, S::BM, fill_rest), n_tiles, band, 32 * S::PER_CU, mt, nt)) return;
     constexpr uint32_t E = sizeof(T);
     const RowTile t = find_row_tile<false>(offsets, G, total, S::BM, mt);
-    if (t.rows == 0 || (t.group == G && !fill_rest)) return;
     const int n0 = nt * S::BN;
     f32x16 acc[S::NB][S::MB] = {};
     if (t.group < G) {
@@ -118,15 +126,14 @@ __global__ __launch_bounds__(S::THREADS) void grouped_rows_kernel(const T* __res
 template <typename S, typename T>
 __global__ __launch_bounds__(S::THREADS) void grouped_weights_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __restrict__ dw,
                                                                      float* __restrict__ partial, const int32_t* __restrict__ offsets, int G,
-                                                                     int64_t total, int K, int N, int height, TileOrder order) {
+                                                                     int64_t total, int K, int N, int height, int n_tiles, int band) {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t mt;
     int nt;
-    if (!tile_of(order, mt, nt)) return;
     const int k_tiles = (K + S::BM - 1) / S::BM;
+    if (!tile_of(count_row_tiles(offsets, G, total, height, false) * k_tiles, n_tiles, band, 32 * S::PER_CU, mt, nt)) return;
     const RowTile t = find_row_tile<true>(offsets, G, total, height, mt / k_tiles);
-    if (t.rows == 0 || t.group == G) return;
     const int k0 = (int)(mt % k_tiles) * S::BM, n0 = nt * S::BN;
     const GroupedOperand a = {(const char*)(x + t.row0 * K + k0), (uint32_t)(K * sizeof(T)), K - k0};
     const GroupedOperand b = {(const char*)(dy + t.row0 * N + n0), (uint32_t)(N * sizeof(T)), N - n0};
@@ -164,17 +171,19 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(const float* __restri
     }
 }
 
+constexpr int BAND = 4;  // row tiles of a band (tile_of)
+
 using Large = GroupedShape<256, 256, 2, 4, 2>;   // one workgroup of eight waves per compute unit
+using Lower = GroupedShape<192, 256, 2, 4, 2>;   // likewise
 using Middle = GroupedShape<128, 128, 2, 2, 2>;  // two of four waves
-using Small = GroupedShape<64, 64, 2, 2, 4>;     // two of four waves, three steps in flight
+using Small = GroupedShape<64, 64, 2, 2, 3>;     // three of four waves, two steps in flight
 
 template <typename S, typename T, bool B_COLUMNS>
 void rows_of(const void* in, const void* w, void* out, const int32_t* offsets, int G, int64_t total, int K, int N, bool fill_rest,
              hipStream_t stream) {
     const int n_tiles = (N + S::BN - 1) / S::BN;
-    const TileOrder order = {row_tiles(G, total, S::BM), n_tiles, 4, n_tiles < 8 ? n_tiles : 8};
-    hipLaunchKernelGGL((grouped_rows_kernel<S, T, B_COLUMNS>), tile_grid(order, S::THREADS), dim3(S::THREADS), 0, stream, (const T*)in, (const T*)w,
-                       (T*)out, offsets, G, total, K, N, fill_rest, order);
+    hipLaunchKernelGGL((grouped_rows_kernel<S, T, B_COLUMNS>), tile_grid(row_tiles(G, total, S::BM) * n_tiles, S::THREADS), dim3(S::THREADS), 0, stream, (const T*)in, (const T*)w,
+                       (T*)out, offsets, G, total, K, N, fill_rest, n_tiles, BAND);
 }
 // Tiles of a launch that have rows, about: every group that can have any ends half a tile early.
 int64_t tiles_with_rows(int G, int64_t total, int columns, int height, int width) {
@@ -191,44 +200,72 @@ void rows(const void* in, const void* w, void* out, const int32_t* offsets, int 
           hipStream_t stream) {
     const int cu = compute_units();
     if constexpr (sizeof(T) == 2)
-        if (tiles_with_rows(G, total, N, 256, 256) >= cu * 6 / 10)
+        if (const int64_t large = tiles_with_rows(G, total, N, 256, 256); large >= cu * 6 / 10 && total >= 96 * (int64_t)(G < total ? G : total)) {
+            // rounds of one tile per compute unit, a Lower one at 3/4 of the work and 1.1 times the time for it
+            const int64_t lower = tiles_with_rows(G, total, N, 192, 256);
+            if (total >= 512 * (int64_t)G && (lower + cu - 1) / cu * 192 * 11 < (large + cu - 1) / cu * 256 * 10)
+                return rows_of<Lower, T, B_COLUMNS>(in, w, out, offsets, G, total, K, N, fill_rest, stream);
             return rows_of<Large, T, B_COLUMNS>(in, w, out, offsets, G, total, K, N, fill_rest, stream);
+        }
     if (tiles_with_rows(G, total, N, 128, 128) >= (sizeof(T) == 2 && B_COLUMNS ? cu : 2 * cu))
         rows_of<Middle, T, B_COLUMNS>(in, w, out, offsets, G, total, K, N, fill_rest, stream);
     else
         rows_of<Small, T, B_COLUMNS>(in, w, out, offsets, G, total, K, N, fill_rest, stream);
 }
 
-// How the weights' gradient is cut: the tile, and the rows per range so that the device is filled about twice.
+// How the weights' gradient is cut: the tile, and the rows per range.
 struct WeightsPlan {
     int tile, height;
     int64_t slots;
 };
-WeightsPlan plan_weights(int64_t total, int K, int N, int dtype) {
-    WeightsPlan p;
-    const auto tiles = [&](int tile) { return (int64_t)((K + tile - 1) / tile) * ((N + tile - 1) / tile); };
-    p.tile = dtype == KUNLUN_BF16 && K > 128 && N > 128 && tiles(256) * (total / 512) >= compute_units() ? 256
-             : tiles(128) * (total / 512 + 1) >= 2 * compute_units() ? 128
-                                                                     : 64;
-    const int64_t resident = (int64_t)compute_units() * (p.tile == 256 ? 1 : 2);
-    int64_t height = total * tiles(p.tile) / (2 * resident);
-    height = (height + 63) / 64 * 64;
-    p.height = (int)(height < 512 ? 512 : height > (1 << 30) ? 1 << 30 : height);
-    p.slots = 2 * total / p.height;  // (a group with a slot has more than one range, so more rows than one)
-    return p;
+// Few ranges leave compute units idle or wait for the longest, many leave partial sums (8 bytes of traffic per weight and range) and
+// short pipelines.  The fastest by a model of that: us per 64 rows of a tile when the device is full, and per tile beyond that, as measured (a
+// Large tile at 1000 TFLOP/s, a Middle one at 850, a Small one at 500; fp32 at 135 and 120), traffic at 5 TB/s.  139 264 rows in 8 groups,
+// 256 -> 768: 85 ranges of 1700 rows in one round of Large tiles, against 175 of 832 in three.
+WeightsPlan plan_weights(int G, int64_t total, int K, int N, int dtype) {
+    struct Tile {
+        int size, per_cu;
+        double step;
+    };
+    static constexpr Tile BF16[] = {{256, 1, 2.05}, {128, 2, 1.27}, {64, 2, 0.52}}, FP32[] = {{128, 2, 8.0}, {64, 2, 2.2}};
+    constexpr double FIXED = 4.0;
+    const double cu = compute_units(), groups = G < total ? G : total, more = groups / 2 + std::sqrt(groups / 3);  // last ranges of groups, hardly ever more
+    WeightsPlan best = {64, 1 << 20, 0};
+    double best_time = -1;
+    for (int i = 0; i < (dtype == KUNLUN_FP32 ? 2 : 3); ++i) {
+        const Tile t = dtype == KUNLUN_FP32 ? FP32[i] : BF16[i];
+        const double tiles = (double)((K + t.size - 1) / t.size) * ((N + t.size - 1) / t.size), resident = cu * t.per_cu;
+        const auto consider = [&](double rows) {
+            const int64_t height = (int64_t)(rows / 64 + 1) * 64;
+            if (height < 256 || height > (1 << 30)) return;
+            const double length = height < total ? height : total, ranges = total / (double)height + more;
+            const double rounds = ranges * tiles / resident, whole = length / 64 * t.step + FIXED;
+            double time = rounds <= 1 ? whole : rounds * (total / ranges / 64 * t.step + FIXED) + whole;
+            if (height < total) time += (total / (double)height + (height * groups < total ? groups / 2 : 0)) * K * N * 8 / 5e6;
+            if (best_time < 0 || time < best_time) {
+                best_time = time;
+                best = {t.size, (int)height, 0};
+            }
+        };
+        for (double rows = 512; rows < 2.0 * total + 512; rows *= 1.25) consider(rows);
+        for (int r = 1; r <= 4; ++r)  // whole rounds
+            if (const double ranges = r * resident / tiles - more; ranges >= 1) consider(total / ranges);
+    }
+    best.slots = 2 * total / best.height;  // (a group with a slot has more than one range, so more rows than one)
+    return best;
 }
 template <typename S, typename T>
 void weights_of(const WeightsPlan& p, const void* x, const void* dy, void* dw, float* partial, const int32_t* offsets, int G, int64_t total, int K,
                 int N, hipStream_t stream) {
     const int n_tiles = (N + S::BN - 1) / S::BN, k_tiles = (K + S::BM - 1) / S::BM;
-    const TileOrder order = {((total + p.height - 1) / p.height + G) * k_tiles, n_tiles, k_tiles < 4 ? k_tiles : 4, n_tiles < 8 ? n_tiles : 8};
-    hipLaunchKernelGGL((grouped_weights_kernel<S, T>), tile_grid(order, S::THREADS), dim3(S::THREADS), 0, stream, (const T*)x, (const T*)dy, (T*)dw,
-                       partial, offsets, G, total, K, N, p.height, order);
+    hipLaunchKernelGGL((grouped_weights_kernel<S, T>), tile_grid(row_tiles(G, total, p.height) * k_tiles * n_tiles, S::THREADS), dim3(S::THREADS), 0, stream, (const T*)x, (const T*)dy, (T*)dw,
+                       partial, offsets, G, total, K, N, p.height, n_tiles,
+                       k_tiles < BAND ? k_tiles : BAND);
 }
 template <typename T>
 void weights(const void* x, const void* dy, void* dw, const int32_t* offsets, int G, int64_t total, int K, int N, int dtype, void* workspace,
              hipStream_t stream) {
-    const WeightsPlan p = plan_weights(total, K, N, dtype);
+    const WeightsPlan p = plan_weights(G, total, K, N, dtype);
     float* partial = (float*)workspace;
     if (total > 0) {
         if constexpr (sizeof(T) == 2)
@@ -251,7 +288,7 @@ hipError_t launch_grouped_linear_fwd(const void* x, const void* w, void* y, cons
 }
 
 size_t grouped_linear_bwd_workspace(int G, int64_t total, int K, int N, int dtype) {
-    return align_up(256 + (size_t)plan_weights(total, K, N, dtype).slots * K * N * sizeof(float), 256);
+    return align_up(256 + (size_t)plan_weights(G, total, K, N, dtype).slots * K * N * sizeof(float), 256);
 }
 
 hipError_t launch_grouped_linear_bwd(const void* x, const void* w, const void* dy, void* dx, void* dw, const int32_t* offsets, int G,

@@ -16,8 +16,6 @@
 
 namespace kunlun {
 
-constexpr int GL_STEP_BYTES = 128;
-template <typename T> constexpr int GL_STEP = GL_STEP_BYTES / sizeof(T);  // contraction values per step
 constexpr uint32_t GL_OUTSIDE = 0x80000000u;     // an offset outside every descriptor
 
 // What a workgroup reads: `base` is the tile's first row (row form) or its first column in the first contraction row (column form).
@@ -28,12 +26,12 @@ struct GroupedOperand {
 };
 
 // DMA of one operand tile: EXTENT rows or columns of C, one step of contraction values.
-template <typename T, int EXTENT, int WAVES, bool COLUMNS>
+template <typename T, int EXTENT, int WAVES, int STEP_BYTES, bool COLUMNS>
 struct GroupedDma {
-    static constexpr int E = sizeof(T), STEP = GL_STEP<T>, BYTES = EXTENT * GL_STEP_BYTES;
+    static constexpr int E = sizeof(T), STEP = STEP_BYTES / E, BYTES = EXTENT * STEP_BYTES;
     static constexpr int LOADS = BYTES / 1024 / WAVES;  // load instructions per wave and step
     static_assert(LOADS >= 1 && LOADS * 1024 * WAVES == BYTES, "a tile splits evenly over the waves");
-    static constexpr int ROW_BYTES = COLUMNS ? EXTENT * E : GL_STEP_BYTES, CHUNKS = ROW_BYTES / 16, ROWS = 1024 / ROW_BYTES;
+    static constexpr int ROW_BYTES = COLUMNS ? EXTENT * E : STEP_BYTES, CHUNKS = ROW_BYTES / 16, ROWS = 1024 / ROW_BYTES;
     static_assert(ROW_BYTES <= 1024, "a load instruction fills whole rows");
     uint32_t voff[LOADS];
     const char* base;
@@ -41,7 +39,7 @@ struct GroupedDma {
     int lane_, wave_;
 
     __device__ static __forceinline__ int swizzle(int row) {
-        if (!COLUMNS) return (row >> 1) & 7;
+        if (!COLUMNS) return STEP_BYTES == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
         return E == 4 ? 0 : ROW_BYTES >= 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
     }
     __device__ __forceinline__ int row_of(int i) const { return (wave_ * LOADS + i) * ROWS + lane_ / CHUNKS; }
@@ -64,7 +62,7 @@ struct GroupedDma {
     // Step k: contraction values STEP k .. of which `left` exist.
     __device__ __forceinline__ void issue(int64_t k, int left, uint32_t lds) const {
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + wave_ * (LOADS * 1024));
-        const char* const from = base + (COLUMNS ? k * STEP * ld : k * GL_STEP_BYTES);
+        const char* const from = base + (COLUMNS ? k * STEP * ld : k * STEP_BYTES);
         const uint32_t bytes = COLUMNS ? (uint32_t)(left < STEP ? left : STEP) * ld : span;
         u32x4 rsrc = make_rsrc_words(from, bytes);
 #pragma unroll
@@ -83,10 +81,10 @@ struct GroupedDma {
 // lane.
 template <typename T> struct GroupedFragOf { typedef bf16x8 type; };
 template <> struct GroupedFragOf<float> { typedef f32x4 type; };
-template <typename T, int EXTENT, bool COLUMNS>
+template <typename T, int EXTENT, int STEP_BYTES, bool COLUMNS>
 struct GroupedFrag {
     typedef typename GroupedFragOf<T>::type Frag;
-    static constexpr int E = sizeof(T), ROW_BYTES = COLUMNS ? EXTENT * E : GL_STEP_BYTES;
+    static constexpr int E = sizeof(T), ROW_BYTES = COLUMNS ? EXTENT * E : STEP_BYTES;
     int at[2];
     __device__ __forceinline__ void init(int lane, int first) {
         const int g = lane >> 5;
@@ -102,7 +100,7 @@ struct GroupedFrag {
             at[0] = 4 * g * ROW_BYTES + (first + (lane & 31)) * 4;
         } else {
             const int row = first + (lane & 31);
-            at[0] = row * ROW_BYTES + ((g ^ ((row >> 1) & 7)) << 4);
+            at[0] = row * ROW_BYTES + ((g ^ (STEP_BYTES == 128 ? (row >> 1) & 7 : (row >> 2) & 3)) << 4);
         }
     }
     // Chunk 2 c + g of the step's contraction values, of the lane's row (column) in block b of 32
@@ -128,33 +126,55 @@ __device__ __forceinline__ f32x16 grouped_mfma(f32x4 a, f32x4 b, f32x16 c) {
     return c;
 }
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int STEP_BYTES_ = 128>
 struct GroupedShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
-    static constexpr int WAVES = WM * WN, THREADS = WAVES * 64;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, STEP_BYTES = STEP_BYTES_;
+    static constexpr int WAVES = WM * WN, THREADS = WAVES * 64, PER_CU = 8 / WAVES;  // two waves per SIMD
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;  // 32 x 32 blocks of a wave
-    static constexpr int A_BYTES = BM * GL_STEP_BYTES, STAGE = A_BYTES + BN * GL_STEP_BYTES;
+    static constexpr int A_BYTES = BM * STEP_BYTES, STAGE = A_BYTES + BN * STEP_BYTES;
     static constexpr int OUT_ROW = NB * 32 * 4 + 16, OUT = WAVES * 32 * OUT_ROW;  // 32 rows of a wave at a time, padded, room for fp32
     static constexpr int LDS = STAGES * STAGE > OUT ? STAGES * STAGE : OUT;
 };
+
+// acc[nb][mb] += the product of one step
+template <typename S, typename T, typename FragA, typename FragB>
+__device__ __forceinline__ void grouped_step(f32x16 (&acc)[S::NB][S::MB], const char* ta, const char* tb, const FragA& frag_a, const FragB& frag_b) {
+#pragma unroll
+    for (int c = 0; c < S::STEP_BYTES / 32; ++c) {
+        typename GroupedFragOf<T>::type fa[S::MB], fb[S::NB];
+#pragma unroll
+        for (int mb = 0; mb < S::MB; ++mb) fa[mb] = frag_a.read(ta, mb, c);
+#pragma unroll
+        for (int nb = 0; nb < S::NB; ++nb) fb[nb] = frag_b.read(tb, nb, c);
+#pragma unroll
+        for (int nb = 0; nb < S::NB; ++nb)
+#pragma unroll
+            for (int mb = 0; mb < S::MB; ++mb) acc[nb][mb] = grouped_mfma(fb[nb], fa[mb], acc[nb][mb]);
+    }
+}
 
 // acc[nb][mb] += the tile's product over `length` contraction values.
 template <typename S, typename T, bool A_COLUMNS, bool B_COLUMNS>
 __device__ __forceinline__ void grouped_product(f32x16 (&acc)[S::NB][S::MB], char* lds, const GroupedOperand& a, const GroupedOperand& b, int length,
                                                 int lane, int wave) {
-    GroupedDma<T, S::BM, S::WAVES, A_COLUMNS> dma_a;
-    GroupedDma<T, S::BN, S::WAVES, B_COLUMNS> dma_b;
+    GroupedDma<T, S::BM, S::WAVES, S::STEP_BYTES, A_COLUMNS> dma_a;
+    GroupedDma<T, S::BN, S::WAVES, S::STEP_BYTES, B_COLUMNS> dma_b;
     dma_a.init(a, lane, wave);
     dma_b.init(b, lane, wave);
-    GroupedFrag<T, S::BM, A_COLUMNS> frag_a;
-    GroupedFrag<T, S::BN, B_COLUMNS> frag_b;
-    frag_a.init(lane, wave / S::WN * (S::BM / S::WM));
-    frag_b.init(lane, wave % S::WN * (S::BN / S::WN));
+    GroupedFrag<T, S::BM, S::STEP_BYTES, A_COLUMNS> frag_a;
+    GroupedFrag<T, S::BN, S::STEP_BYTES, B_COLUMNS> frag_b;
+    const int row0 = wave / S::WN * (S::BM / S::WM), col0 = wave % S::WN * (S::BN / S::WN);
+    frag_a.init(lane, row0);
+    frag_b.init(lane, col0);
+    // Whether any of the wave's rows and columns exist (asked for Small tiles only: 9973 rows, 328 -> 200, fp32: 27 -> 23 us; the branch costs
+    // the larger ones up to 7 % and leaves little out)
+    const bool live = S::BM > 64 || (row0 < a.valid && col0 < b.valid);
     constexpr int LOADS = decltype(dma_a)::LOADS + decltype(dma_b)::LOADS;
-    const int steps = (length + GL_STEP<T> - 1) / GL_STEP<T>;
+    constexpr int STEP = decltype(dma_a)::STEP;
+    const int steps = (length + STEP - 1) / STEP;
     const uint32_t lds0 = lds_address(lds);
     auto issue = [&](int k, int stage) {
-        const int left = length - k * GL_STEP<T>;
+        const int left = length - k * STEP;
         dma_a.issue(k, left, lds0 + stage * S::STAGE);
         dma_b.issue(k, left, lds0 + stage * S::STAGE + S::A_BYTES);
     };
@@ -168,20 +188,8 @@ __device__ __forceinline__ void grouped_product(f32x16 (&acc)[S::NB][S::MB], cha
         __syncthreads();  // step k has arrived; every wave is done with the stage of step k - 1
         if (k + S::STAGES - 1 < steps) issue(k + S::STAGES - 1, stage == 0 ? S::STAGES - 1 : stage - 1);
         const char* ta = lds + stage * S::STAGE;
-        const char* tb = ta + S::A_BYTES;
         stage = stage == S::STAGES - 1 ? 0 : stage + 1;
-#pragma unroll
-        for (int c = 0; c < GL_STEP_BYTES / 32; ++c) {
-            typename GroupedFragOf<T>::type fa[S::MB], fb[S::NB];
-#pragma unroll
-            for (int mb = 0; mb < S::MB; ++mb) fa[mb] = frag_a.read(ta, mb, c);
-#pragma unroll
-            for (int nb = 0; nb < S::NB; ++nb) fb[nb] = frag_b.read(tb, nb, c);
-#pragma unroll
-            for (int nb = 0; nb < S::NB; ++nb)
-#pragma unroll
-                for (int mb = 0; mb < S::MB; ++mb) acc[nb][mb] = grouped_mfma(fb[nb], fa[mb], acc[nb][mb]);
-        }
+        if (live) grouped_step<S, T>(acc, ta, ta + S::A_BYTES, frag_a, frag_b);
     }
     __syncthreads();  // every wave is done with the ring: it stages the output next
 }
@@ -212,6 +220,35 @@ __device__ __forceinline__ void grouped_store(const f32x16 (&acc)[S::NB][S::MB],
             const int row = i * PER_PASS + lane / PIECES, piece = lane % PIECES;
             const u32x4 v = *(const u32x4*)(mine + row * S::OUT_ROW + piece * 16);
             const int m = row0 + 32 * mb + row, n = col0 + piece * (16 / E);
+            if (m < rows && n < columns) __builtin_nontemporal_store(v, (u32x4*)(out + (int64_t)m * ld + n));
+        }
+    }
+}
+
+// The same for bf16 tiles of waves of 64 columns, through 4 KB of LDS per wave that are no part of the ring: rows of 128 bytes whose
+// 16-byte chunk ^= (row / 2) % 8 instead of padding.
+template <typename S>
+__device__ __forceinline__ void grouped_store_beside(const f32x16 (&acc)[S::NB][S::MB], char* mine, bf16_t* out, int64_t ld, int rows, int columns,
+                                                     int lane, int wave) {
+    static_assert(S::NB == 2, "a wave's rows are 128 bytes");
+    const int r = lane & 31, g = lane >> 5;
+    const int row0 = wave / S::WN * (S::BM / S::WM), col0 = wave % S::WN * (S::BN / S::WN);
+#pragma unroll
+    for (int mb = 0; mb < S::MB; ++mb) {
+#pragma unroll
+        for (int nb = 0; nb < S::NB; ++nb)
+#pragma unroll
+            for (int vg = 0; vg < 4; ++vg) {
+                bf16x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (bf16_t)acc[nb][mb][4 * vg + e];
+                *(bf16x4*)(mine + r * 128 + (((4 * nb + vg) ^ ((r >> 1) & 7)) << 4) + g * 8) = o;
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + lane / 8, piece = lane % 8;
+            const u32x4 v = *(const u32x4*)(mine + row * 128 + ((piece ^ ((row >> 1) & 7)) << 4));
+            const int m = row0 + 32 * mb + row, n = col0 + piece * 8;
             if (m < rows && n < columns) *(u32x4*)(out + (int64_t)m * ld + n) = v;
         }
     }
