@@ -68,7 +68,22 @@ constexpr int SORT_TILE = SORT_THREADS * SORT_KEYS;
 constexpr int DIGIT_MOST = 10;  // bits of a digit: two passes up to a million table rows
 constexpr int BINS_MOST = 1 << DIGIT_MOST;
 constexpr int64_t SORT_RANGES = 512;  // most ranges of a pass
+constexpr int64_t FILL_BLOCKS = 192;
 constexpr unsigned SCAN_RANGES = 64;  // from more on a launch of its own scans the counts
+
+// The workgroups of a sorting launch behind its first `ranges` ones set a part of the table's gradient to zero meanwhile.
+struct Fill {
+    char* base;
+    int64_t begin, end;  // bytes, multiples of 16 but for the end of the last part
+};
+__device__ __forceinline__ void fill_zero(const Fill& f, int block, int blocks) {
+    const u32x4_any zero = {0, 0, 0, 0};
+    for (int64_t i = f.begin + ((int64_t)block * SORT_THREADS + threadIdx.x) * 16; i < f.end; i += (int64_t)blocks * SORT_THREADS * 16) {
+        if (i + 16 <= f.end) __builtin_nontemporal_store(zero, (u32x4_any*)(f.base + i));
+        else
+            for (int64_t k = i; k < f.end; k += 2) *(uint16_t*)(f.base + k) = 0;
+    }
+}
 
 // Where a pass reads: the ids themselves (first pass) or the pairs of the pass before.  An id outside the table sorts as
 // `rows`, behind every id of the table.
@@ -81,8 +96,9 @@ __device__ __forceinline__ uint2 pair_at(const ID* ids, const uint2* pairs, int6
 
 template <typename ID>
 __global__ __launch_bounds__(SORT_THREADS) void digit_count_kernel(const ID* __restrict__ ids, const uint2* __restrict__ pairs,
-                                                                   uint32_t* __restrict__ counts, int64_t n, int64_t per_range, uint32_t rows,
-                                                                   int shift, int bits) {
+                                                                   uint32_t* __restrict__ counts, int64_t n, int64_t per_range, int ranges,
+                                                                   uint32_t rows, int shift, int bits, Fill fill) {
+    if ((int)blockIdx.x >= ranges) return fill_zero(fill, blockIdx.x - ranges, gridDim.x - ranges);
     __shared__ uint32_t count[BINS_MOST];
     const int bins = 1 << bits;
     for (int d = threadIdx.x; d < bins; d += SORT_THREADS) count[d] = 0;
@@ -226,8 +242,9 @@ template <typename ID>
 __global__ __launch_bounds__(SORT_THREADS) void digit_move_kernel(const ID* __restrict__ ids, const uint2* __restrict__ pairs,
                                                                   const uint32_t* __restrict__ counts, const uint32_t* __restrict__ totals,
                                                                   uint2* __restrict__ out, uint32_t* __restrict__ keys_out,
-                                                                  uint32_t* __restrict__ positions_out, int64_t n, int64_t per_range, uint32_t rows,
-                                                                  int shift, int bits) {
+                                                                  uint32_t* __restrict__ positions_out, int64_t n, int64_t per_range, int ranges,
+                                                                  uint32_t rows, int shift, int bits, Fill fill) {
+    if ((int)blockIdx.x >= ranges) return fill_zero(fill, blockIdx.x - ranges, gridDim.x - ranges);
     __shared__ SortSpaceLds s;
     __shared__ uint32_t to[BINS_MOST];  // where the range's next pair of a digit goes
     const int bins = 1 << bits;
@@ -239,13 +256,13 @@ __global__ __launch_bounds__(SORT_THREADS) void digit_move_kernel(const ID* __re
             const uint2 all = *(const uint2*)(totals + d0), mine = *(const uint2*)(counts + (int64_t)blockIdx.x * bins + d0);
             at[0] = all.x; at[1] = all.y; before[0] = mine.x; before[1] = mine.y;
         } else {
-            for (int r0 = 0; r0 < (int)gridDim.x; r0 += SCAN_FETCH) {
+            for (int r0 = 0; r0 < ranges; r0 += SCAN_FETCH) {
                 uint2 c[SCAN_FETCH];
 #pragma unroll
-                for (int u = 0; u < SCAN_FETCH; ++u) c[u] = *(const uint2*)(counts + (int64_t)(r0 + u < (int)gridDim.x ? r0 + u : r0) * bins + d0);
+                for (int u = 0; u < SCAN_FETCH; ++u) c[u] = *(const uint2*)(counts + (int64_t)(r0 + u < ranges ? r0 + u : r0) * bins + d0);
 #pragma unroll
                 for (int u = 0; u < SCAN_FETCH; ++u) {
-                    if (r0 + u < (int)gridDim.x) { at[0] += c[u].x; at[1] += c[u].y; }
+                    if (r0 + u < ranges) { at[0] += c[u].x; at[1] += c[u].y; }
                     if (r0 + u < (int)blockIdx.x) { before[0] += c[u].x; before[1] += c[u].y; }
                 }
             }
@@ -283,7 +300,9 @@ __global__ __launch_bounds__(SORT_THREADS) void digit_move_kernel(const ID* __re
 
 template <typename ID>
 __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const ID* __restrict__ ids, uint32_t* __restrict__ keys_out,
-                                                                  uint32_t* __restrict__ positions_out, int n, uint32_t rows, int passes, int bits) {
+                                                                  uint32_t* __restrict__ positions_out, int n, uint32_t rows, int passes, int bits,
+                                                                  Fill fill) {
+    if (blockIdx.x > 0) return fill_zero(fill, blockIdx.x - 1, gridDim.x - 1);
     __shared__ SortSpaceLds s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint2 pair[SORT_KEYS];
@@ -309,6 +328,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const ID* __re
 
 constexpr int ADD_FETCH = 8;  // rows in flight per lane group
 constexpr int JOIN_FETCH = 8, JOIN_ALONE = 16;  // partial sums in flight; ranges of a run that one lane group adds
+constexpr int JOIN_SUMS = 16;                   // most parts of a longer one that are added one after another
 constexpr int ZERO_ROWS = 64; // table rows that a workgroup searches for
 
 __device__ __forceinline__ int64_t first_at_least(const uint32_t* keys, int64_t lo, int64_t hi, uint32_t key) {
@@ -475,10 +495,27 @@ __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t*
 #pragma unroll
         for (int j = 0; j < W; ++j) parts[threadIdx.x * W + j] = acc[j];
         __syncthreads();
-        if (group == 0) {
-            for (int g = 1; g < groups; ++g)
+        const auto add_parts = [&](int g0, int g1) {
+            for (int g = g0; g < g1; ++g)
 #pragma unroll
                 for (int j = 0; j < W; ++j) acc[j] += parts[(g * lanes + lane) * W + j];
+        };
+        const int sums = groups < JOIN_SUMS ? groups : JOIN_SUMS, span = groups / sums;
+        if (span > 1) {  // (many narrow lane groups: their parts in two steps)
+            const int g0 = group * span;
+            if (group < sums) {
+#pragma unroll
+                for (int j = 0; j < W; ++j) acc[j] = 0.f;
+                add_parts(g0, g0 + span);
+            }
+            __syncthreads();
+            if (group < sums)
+#pragma unroll
+                for (int j = 0; j < W; ++j) parts[threadIdx.x * W + j] = acc[j];
+            __syncthreads();
+        }
+        if (group == 0) {
+            add_parts(1, sums);
             finish(acc, key_of[w]);
         }
     }
@@ -501,17 +538,18 @@ void embedding_fwd(const void* table, const void* ids, void* out, int64_t n, int
     else embedding_fwd<T, W, int32_t>(table, ids, out, n, rows, D, scale, stream);
 }
 
-// Pairs per lane group: ranges enough to fill the device (about 16 waves per compute unit of them), long ones otherwise, so that
-// few runs cross a range and leave partial sums.
-constexpr int64_t CHUNK_LEAST = 8, RANGES_MOST = 16384;
-int64_t add_chunk(int64_t n) {
+// Pairs per lane group: ranges enough to fill the device (16 waves per compute unit of them), long ones otherwise, so that few runs
+// cross a range and leave partial sums (1.1 million rows of 64, eight lanes each: 119 us with 8942 ranges, 109 us with 35 769).
+constexpr int64_t CHUNK_LEAST = 8;
+int64_t ranges_most(int lanes) { return lanes < 32 ? ((int64_t)1 << 19) / lanes : 1 << 14; }
+int64_t add_chunk(int64_t n, int lanes) {
     int64_t chunk = CHUNK_LEAST;
-    while ((n + chunk - 1) / chunk > RANGES_MOST) chunk *= 2;
+    while ((n + chunk - 1) / chunk > ranges_most(lanes)) chunk *= 2;
     return chunk;
 }
-int64_t ranges_at_most(int64_t n) {
+int64_t ranges_at_most(int64_t n, int lanes) {
     const int64_t r = (n + CHUNK_LEAST - 1) / CHUNK_LEAST;
-    return r < RANGES_MOST ? r : RANGES_MOST;
+    return r < ranges_most(lanes) ? r : ranges_most(lanes);
 }
 
 struct SortSpace {
@@ -530,19 +568,29 @@ struct SortSpace {
         counts = (uint32_t*)take((size_t)(tiles < SORT_RANGES ? tiles : SORT_RANGES) * BINS_MOST * 4);
         totals = (uint32_t*)take(BINS_MOST * 4);
         const int W = dtype == KUNLUN_FP32 ? piece_width<float>(D) : piece_width<bf16_t>(D);
-        partial = (float*)take((size_t)ranges_at_most(n) * 2 * pieces_per_row(D, W) * W * 4);
+        const int pieces = pieces_per_row(D, W);
+        partial = (float*)take((size_t)ranges_at_most(n, lanes_per_row(pieces)) * 2 * pieces * W * 4);
         bytes = at;
     }
 };
 
+// fill_bytes > 0: the launches set that much of d_table to zero as well, each an equal part.
 template <typename ID>
-void sort_ids(const void* ids, const SortSpace& s, int64_t n, int64_t rows, hipStream_t stream) {
+void sort_ids(const void* ids, const SortSpace& s, int64_t n, int64_t rows, void* d_table, int64_t fill_bytes, hipStream_t stream) {
     int bits = 1;
     while (rows >> bits) ++bits;  // keys are 0 .. rows
     const int passes = (bits + DIGIT_MOST - 1) / DIGIT_MOST, digit = (bits + passes - 1) / passes;
+    const int launches = n <= SORT_TILE ? 1 : 2 * passes;
+    const int64_t part = (fill_bytes + launches * 16 - 1) / (launches * 16) * 16;
+    const unsigned fill_blocks = (unsigned)(part / (SORT_THREADS * 64) < FILL_BLOCKS ? (part + SORT_THREADS * 64 - 1) / (SORT_THREADS * 64) : FILL_BLOCKS);
+    int launched = 0;
+    const auto fill = [&] {
+        const int64_t begin = launched++ * part, end = begin + part;
+        return Fill{(char*)d_table, begin < fill_bytes ? begin : fill_bytes, end < fill_bytes ? end : fill_bytes};
+    };
     if (n <= SORT_TILE) {
-        hipLaunchKernelGGL(sort_small_kernel<ID>, dim3(1), dim3(SORT_THREADS), 0, stream, (const ID*)ids, s.keys, s.positions, (int)n, (uint32_t)rows, passes,
-                           digit);
+        hipLaunchKernelGGL(sort_small_kernel<ID>, dim3(1 + fill_blocks), dim3(SORT_THREADS), 0, stream, (const ID*)ids, s.keys, s.positions, (int)n, (uint32_t)rows, passes,
+                           digit, fill());
         return;
     }
     const int64_t tiles = (n + SORT_TILE - 1) / SORT_TILE, per_range = (tiles + SORT_RANGES - 1) / SORT_RANGES * SORT_TILE;
@@ -552,22 +600,24 @@ void sort_ids(const void* ids, const SortSpace& s, int64_t n, int64_t rows, hipS
     uint32_t* const totals = ranges > SCAN_RANGES ? s.totals : nullptr;
     for (int p = 0; p < passes; ++p) {
         const uint2* from = p ? s.pairs[(p + 1) & 1] : nullptr;
-        hipLaunchKernelGGL(digit_count_kernel<ID>, dim3(ranges), dim3(SORT_THREADS), 0, stream, (const ID*)ids, from, s.counts, n, per_range,
-                           (uint32_t)rows, p * digit, digit);
+        hipLaunchKernelGGL(digit_count_kernel<ID>, dim3(ranges + fill_blocks), dim3(SORT_THREADS), 0, stream, (const ID*)ids, from, s.counts, n,
+                           per_range, (int)ranges, (uint32_t)rows, p * digit, digit, fill());
         if (totals)
             hipLaunchKernelGGL(digit_scan_kernel, dim3((unsigned)((bins + 31) / 32)), dim3(32 * SCAN_PARTS), 0, stream, s.counts, totals, (int)ranges,
                                bins);
-        hipLaunchKernelGGL(digit_move_kernel<ID>, dim3(ranges), dim3(SORT_THREADS), 0, stream, (const ID*)ids, from, s.counts, totals,
-                           p + 1 < passes ? s.pairs[p & 1] : nullptr, s.keys, s.positions, n, per_range, (uint32_t)rows, p * digit, digit);
+        hipLaunchKernelGGL(digit_move_kernel<ID>, dim3(ranges + fill_blocks), dim3(SORT_THREADS), 0, stream, (const ID*)ids, from, s.counts, totals,
+                           p + 1 < passes ? s.pairs[p & 1] : nullptr, s.keys, s.positions, n, per_range, (int)ranges, (uint32_t)rows,
+                           p * digit, digit, fill());
     }
 }
 
 template <typename T, int W>
-void embedding_bwd(const void* d_out, const SortSpace& s, void* d_table, int64_t n, int64_t rows, int D, float scale, hipStream_t stream) {
+void embedding_bwd(const void* d_out, const SortSpace& s, void* d_table, int64_t n, int64_t rows, int D, float scale, bool filled,
+                   hipStream_t stream) {
     const int pieces = pieces_per_row(D, W), lanes = lanes_per_row(pieces), groups = THREADS / lanes;
-    const int64_t chunk = add_chunk(n), ranges = (n + chunk - 1) / chunk;
+    const int64_t chunk = add_chunk(n, lanes), ranges = (n + chunk - 1) / chunk;
     const int64_t add_blocks = (ranges + groups - 1) / groups, zero_all = (rows + ZERO_ROWS - 1) / ZERO_ROWS;
-    const int64_t zero_blocks = zero_all < GRID_MOST ? zero_all : GRID_MOST;
+    const int64_t zero_blocks = filled ? 0 : zero_all < GRID_MOST ? zero_all : GRID_MOST;
     const unsigned tiles = (unsigned)((pieces + 63) / 64);
     hipLaunchKernelGGL((embedding_add_kernel<T, W>), dim3((unsigned)(add_blocks + zero_blocks), tiles), dim3(THREADS), 0, stream, (const T*)d_out,
                        s.keys, s.positions, (T*)d_table, s.partial, n, (uint32_t)rows, D, scale, lanes, chunk, add_blocks);
@@ -592,19 +642,26 @@ hipError_t launch_embedding_fwd(const void* table, const void* ids, void* out, i
 
 size_t embedding_bwd_workspace(int64_t n, int D, int dtype) { return SortSpace(nullptr, n, D, dtype).bytes; }
 
+// A gradient up to here is set to zero by the sorting launches, which leave most of the device idle, and rows with ids are written over
+// (139 264 rows of 256 into 200 000: 83 -> 78 us, into 500 000: 107 -> 95; 640 into 500 000: 66 -> 54); beyond, the rows without ids are
+// found among the sorted ones.
+constexpr int64_t FILL_MOST = (int64_t)256 << 20;
+
 hipError_t launch_embedding_bwd(const void* d_out, const void* ids, void* d_table, int64_t n, int64_t rows, int D, float scale,
                                 int id_bytes, int dtype, void* workspace, hipStream_t stream) {
     const SortSpace s((char*)workspace, n, D, dtype);
+    const int64_t bytes = rows * D * (dtype == KUNLUN_FP32 ? 4 : 2);
+    const bool filled = n > 0 && bytes <= FILL_MOST;
     if (n > 0) {
-        if (id_bytes == 8) sort_ids<int64_t>(ids, s, n, rows, stream);
-        else sort_ids<int32_t>(ids, s, n, rows, stream);
+        if (id_bytes == 8) sort_ids<int64_t>(ids, s, n, rows, d_table, filled ? bytes : 0, stream);
+        else sort_ids<int32_t>(ids, s, n, rows, d_table, filled ? bytes : 0, stream);
     }
     if (dtype == KUNLUN_FP32) {
-        if (piece_width<float>(D) == 4) embedding_bwd<float, 4>(d_out, s, d_table, n, rows, D, scale, stream);
-        else embedding_bwd<float, 1>(d_out, s, d_table, n, rows, D, scale, stream);
+        if (piece_width<float>(D) == 4) embedding_bwd<float, 4>(d_out, s, d_table, n, rows, D, scale, filled, stream);
+        else embedding_bwd<float, 1>(d_out, s, d_table, n, rows, D, scale, filled, stream);
     } else {
-        if (piece_width<bf16_t>(D) == 8) embedding_bwd<bf16_t, 8>(d_out, s, d_table, n, rows, D, scale, stream);
-        else embedding_bwd<bf16_t, 1>(d_out, s, d_table, n, rows, D, scale, stream);
+        if (piece_width<bf16_t>(D) == 8) embedding_bwd<bf16_t, 8>(d_out, s, d_table, n, rows, D, scale, filled, stream);
+        else embedding_bwd<bf16_t, 1>(d_out, s, d_table, n, rows, D, scale, filled, stream);
     }
     return hipGetLastError();
 }

@@ -16,20 +16,47 @@ namespace {
 constexpr int THREADS = 256;
 constexpr int VALUES_PER_LANE = 32;  // most values of a row that a lane holds where a wave holds rows
 
-// Sum over the lanes of a group (lanes a power of two up to 64), or over the whole workgroup (WIDE).
-template <bool WIDE>
-__device__ __forceinline__ float group_sum(float x, int lanes, float* scratch) {
-    for (int o = lanes / 2; o > 0; o /= 2) x += __shfl_xor(x, o);
-    if constexpr (WIDE) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) scratch[wave] = x;
-        __syncthreads();
-        x = scratch[0];
-#pragma unroll
-        for (int w = 1; w < THREADS / 64; ++w) x += scratch[w];
+// x + the value of x in the lane that CTRL names, by a vector operation (a shuffle would take an LDS round trip).
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float x) {
+    return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// Sum over the lanes of a group (a power of two up to 64; all lanes of the wave take part), the same in all of them.
+__device__ __forceinline__ float lanes_sum(float x, int lanes) {
+    if (lanes > 1) x = add_dpp<0xb1>(x);   // lane ^ 1
+    if (lanes > 2) x = add_dpp<0x4e>(x);   // lane ^ 2
+    if (lanes > 4) x = add_dpp<0x141>(x);  // mirrored in 8 lanes, whose fours are equal by now
+    if (lanes > 8) x = add_dpp<0x140>(x);  // mirrored in 16
+    if (lanes > 16) {
+        const unsigned u = __builtin_bit_cast(unsigned, x);
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+    }
+    if (lanes > 32) {
+        const unsigned u = __builtin_bit_cast(unsigned, x);
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
     }
     return x;
+}
+// Sums of N values over a group, or over the whole workgroup (WIDE).
+template <bool WIDE, int N>
+__device__ __forceinline__ void group_sums(float (&x)[N], int lanes, float (*scratch)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = lanes_sum(x[i], WIDE ? 64 : lanes);
+    if constexpr (WIDE) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) scratch[threadIdx.x >> 6][i] = x[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = scratch[0][i];
+#pragma unroll
+            for (int w = 1; w < THREADS / 64; ++w) x[i] += scratch[w][i];
+        }
+    }
 }
 
 // Where a lane's pieces lie: piece c of the row starts at at(c); the first dup(c) values of it belong to the piece before (all W: no piece)
@@ -52,7 +79,7 @@ template <typename T, int W, int VPL, bool WIDE>
 __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
                                                            T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, int64_t rows,
                                                            int D, float eps, int lanes) {
-    __shared__ float scratch[THREADS / 64];
+    __shared__ float scratch[THREADS / 64][1];
     const int per_row = WIDE ? THREADS : lanes, lane = threadIdx.x % per_row, groups = THREADS / per_row;
     const Pieces<W, VPL> at(lane, per_row, D);
     Piece<T, W> w[VPL], b[VPL];
@@ -69,21 +96,23 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(const T* __restrict__
         Piece<T, W> v[VPL];
 #pragma unroll
         for (int i = 0; i < VPL; ++i) v[i] = load_piece<T, W>(x + r * D + at.at[i]);
-        float s = 0.f;
+        float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < VPL; ++i)
 #pragma unroll
-            for (int j = 0; j < W; ++j) s += j >= at.dup[i] ? to_float(v[i].v[j]) : 0.f;
-        const float m = group_sum<WIDE>(s, WIDE ? 64 : lanes, scratch) / n;
-        s = 0.f;
+            for (int j = 0; j < W; ++j) s[0] += j >= at.dup[i] ? to_float(v[i].v[j]) : 0.f;
+        group_sums<WIDE>(s, lanes, scratch);
+        const float m = s[0] / n;
+        s[0] = 0.f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i)
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 const float d = to_float(v[i].v[j]) - m;
-                s += j >= at.dup[i] ? d * d : 0.f;
+                s[0] += j >= at.dup[i] ? d * d : 0.f;
             }
-        const float rs = 1.f / sqrtf(group_sum<WIDE>(s, WIDE ? 64 : lanes, scratch) / n + eps);
+        group_sums<WIDE>(s, lanes, scratch);
+        const float rs = 1.f / sqrtf(s[0] / n + eps);
         if (mine >= rows) continue;
         if (lane == 0) {
             if (mean) mean[r] = m;
@@ -111,7 +140,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const T* __restrict__
                                                            const float* __restrict__ mean, const float* __restrict__ rstd, T* __restrict__ dx,
                                                            float* __restrict__ partial, int64_t rows, int D, int lanes) {
     extern __shared__ float columns[];  // [groups][D], one of the two sums at a time
-    __shared__ float scratch[THREADS / 64];
+    __shared__ float scratch[THREADS / 64][2];
     const int per_row = WIDE ? THREADS : lanes, lane = threadIdx.x % per_row, groups = THREADS / per_row, group = threadIdx.x / per_row;
     const Pieces<W, VPL> at(lane, per_row, D);
     Piece<T, W> w[VPL];
@@ -124,42 +153,58 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const T* __restrict__
     }
     const float n = (float)D;
     const int64_t step = (int64_t)gridDim.x * groups;
-    for (int64_t r0 = (int64_t)blockIdx.x * groups; r0 < rows; r0 += step) {
-        const int64_t mine = r0 + group, r = mine < rows ? mine : rows - 1;
-        const bool ok = mine < rows;
-        const float m = mean[r], rs = rstd[r];
+    constexpr bool AHEAD = VPL * W <= 16;  // registers to spare: the next row is under way while one is computed
+    struct Row {
         Piece<T, W> v[VPL], d[VPL];
+        float m, rs;
+    };
+    auto load = [&](Row& row, int64_t r0) {
+        const int64_t r = r0 + group < rows ? r0 + group : rows - 1;
+        row.m = mean[r];
+        row.rs = rstd[r];
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            v[i] = load_piece<T, W>(x + r * D + at.at[i]);
-            d[i] = load_piece<T, W>(dy + r * D + at.at[i]);
+            row.v[i] = load_piece<T, W>(x + r * D + at.at[i]);
+            row.d[i] = load_piece<T, W>(dy + r * D + at.at[i]);
         }
-        float sg = 0.f, sgh = 0.f;
+    };
+    Row now;
+    if (AHEAD) load(now, (int64_t)blockIdx.x * groups);
+    for (int64_t r0 = (int64_t)blockIdx.x * groups; r0 < rows; r0 += step) {
+        const int64_t r = r0 + group;
+        const bool ok = r < rows;
+        Row next;
+        if (AHEAD) load(next, r0 + step);
+        else load(now, r0);
+        const float m = now.m, rs = now.rs;
+        float sums[2] = {0.f, 0.f};  // of g, of g h
 #pragma unroll
         for (int i = 0; i < VPL; ++i)
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                const float h = (to_float(v[i].v[j]) - m) * rs, t = to_float(d[i].v[j]), g = weight ? t * to_float(w[i].v[j]) : t;
+                const float h = (to_float(now.v[i].v[j]) - m) * rs, t = to_float(now.d[i].v[j]), g = weight ? t * to_float(w[i].v[j]) : t;
                 const bool counts = j >= at.dup[i];
-                sg += counts ? g : 0.f;
-                sgh += counts ? g * h : 0.f;
+                sums[0] += counts ? g : 0.f;
+                sums[1] += counts ? g * h : 0.f;
                 dw[i][j] += ok ? t * h : 0.f;
                 db[i][j] += ok ? t : 0.f;
             }
-        if (!dx) continue;
-        sg = group_sum<WIDE>(sg, WIDE ? 64 : lanes, scratch) / n;
-        sgh = group_sum<WIDE>(sgh, WIDE ? 64 : lanes, scratch) / n;
+        if (dx) {
+            group_sums<WIDE>(sums, lanes, scratch);
+            const float sg = sums[0] / n, sgh = sums[1] / n;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            if (!ok || !at.has(i)) continue;
-            Piece<T, W> o;
+            for (int i = 0; i < VPL; ++i) {
+                if (!ok || !at.has(i)) continue;
+                Piece<T, W> o;
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const float h = (to_float(v[i].v[j]) - m) * rs, t = to_float(d[i].v[j]), g = weight ? t * to_float(w[i].v[j]) : t;
-                o.v[j] = from_float<T>((g - sg - h * sgh) * rs);
+                for (int j = 0; j < W; ++j) {
+                    const float h = (to_float(now.v[i].v[j]) - m) * rs, t = to_float(now.d[i].v[j]), g = weight ? t * to_float(w[i].v[j]) : t;
+                    o.v[j] = from_float<T>((g - sg - h * sgh) * rs);
+                }
+                store_piece<T, W>(dx + r * D + at.at[i], o);
             }
-            store_piece<T, W>(dx + r * D + at.at[i], o);
         }
+        if (AHEAD) now = next;
     }
     if (!partial) return;
 #pragma unroll
@@ -229,7 +274,9 @@ RowPlan plan_row(int D, int elt) {
     return p;
 }
 
-constexpr int BWD_BLOCKS = 512;  // workgroups of the backward launch (two per compute unit), each with a row of partial sums
+// Workgroups of the backward launch, each with a row of partial sums: two per compute unit, four where rows are narrow and what a
+// workgroup waits for counts more than the partial sums do
+int64_t bwd_blocks(int D) { return D <= 512 ? 1024 : 512; }
 int64_t blocks_of(const RowPlan& p, int64_t rows, int64_t most) {
     const int groups = p.wide ? 1 : THREADS / p.lanes;
     const int64_t all = (rows + groups - 1) / groups;
@@ -246,7 +293,7 @@ template <typename T, int W, int VPL, bool WIDE>
 void norm_bwd(const RowPlan& p, const void* x, const void* weight, const void* dy, const float* mean, const float* rstd, void* dx, float* partial,
               int64_t rows, int D, hipStream_t stream) {
     const size_t lds = p.wide || !partial ? 0 : (size_t)(THREADS / p.lanes) * D * sizeof(float);
-    hipLaunchKernelGGL((norm_bwd_kernel<T, W, VPL, WIDE>), dim3((unsigned)blocks_of(p, rows, BWD_BLOCKS)), dim3(THREADS), lds, stream, (const T*)x,
+    hipLaunchKernelGGL((norm_bwd_kernel<T, W, VPL, WIDE>), dim3((unsigned)blocks_of(p, rows, bwd_blocks(D))), dim3(THREADS), lds, stream, (const T*)x,
                        (const T*)weight, (const T*)dy, mean, rstd, (T*)dx, partial, rows, D, p.lanes);
 }
 
@@ -291,7 +338,7 @@ hipError_t launch_layer_norm_fwd(const void* x, const void* weight, const void* 
 }
 
 size_t layer_norm_bwd_workspace(int64_t rows, int D, int dtype) {
-    const int64_t parts = blocks_of(plan_row(D, dtype == KUNLUN_FP32 ? 4 : 2), rows, BWD_BLOCKS);
+    const int64_t parts = blocks_of(plan_row(D, dtype == KUNLUN_FP32 ? 4 : 2), rows, bwd_blocks(D));
     return align_up((size_t)(parts > 0 ? parts : 1) * 2 * D * sizeof(float), 256);
 }
 
@@ -299,7 +346,7 @@ hipError_t launch_layer_norm_bwd(const void* x, const void* weight, const void* 
                                  void* dw, void* db, int64_t rows, int D, int dtype, void* workspace, hipStream_t stream) {
     const RowPlan p = plan_row(D, dtype == KUNLUN_FP32 ? 4 : 2);
     float* partial = dw || db ? (float*)workspace : nullptr;
-    const int parts = (int)blocks_of(p, rows, BWD_BLOCKS);
+    const int parts = (int)blocks_of(p, rows, bwd_blocks(D));
     if (rows > 0) {
         const hipError_t e = dispatch_bwd(p, dtype, x, weight, dy, mean, rstd, dx, partial, rows, D, stream);
         if (e != hipSuccess) return e;
