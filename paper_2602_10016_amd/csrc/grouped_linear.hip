@@ -126,7 +126,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_rows_kernel(const T* __
 template <typename S, typename T>
 __global__ __launch_bounds__(S::THREADS) void grouped_weights_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __restrict__ dw,
                                                                      float* __restrict__ partial, const int32_t* __restrict__ offsets, int G,
-                                                                     int64_t total, int K, int N, int height, int n_tiles, int band) {
+                                                                     int64_t total, int K, int N, int height, int64_t slots, int n_tiles, int band) {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int64_t mt;
@@ -134,6 +134,7 @@ __global__ __launch_bounds__(S::THREADS) void grouped_weights_kernel(const T* __
     const int k_tiles = (K + S::BM - 1) / S::BM;
     if (!tile_of(count_row_tiles(offsets, G, total, height, false) * k_tiles, n_tiles, band, 32 * S::PER_CU, mt, nt)) return;
     const RowTile t = find_row_tile<true>(offsets, G, total, height, mt / k_tiles);
+    if (t.slot >= slots) return;  // (offsets that are none)
     const int k0 = (int)(mt % k_tiles) * S::BM, n0 = nt * S::BN;
     const GroupedOperand a = {(const char*)(x + t.row0 * K + k0), (uint32_t)(K * sizeof(T)), K - k0};
     const GroupedOperand b = {(const char*)(dy + t.row0 * N + n0), (uint32_t)(N * sizeof(T)), N - n0};
@@ -146,23 +147,32 @@ __global__ __launch_bounds__(S::THREADS) void grouped_weights_kernel(const T* __
 }
 
 // dw[g] where group g has not exactly one range: the sum of its slots in order, zeros without any.  Four values per thread.
+constexpr int SLOT_FETCH = 8;  // loads in flight
 template <typename T>
 __global__ __launch_bounds__(256) void grouped_join_kernel(const float* __restrict__ partial, T* __restrict__ dw,
-                                                           const int32_t* __restrict__ offsets, int G, int64_t total, int64_t per_group, int height) {
+                                                           const int32_t* __restrict__ offsets, int G, int64_t total, int64_t per_group, int height,
+                                                           int64_t slots) {
     const int g = blockIdx.y;
     int64_t lo;
     int len, slot = 0;
     for (int g0 = 0; g0 < g; g0 += 64) {
         int n = tiles_of(offsets, G, total, height, g0 + (threadIdx.x & 63), lo, len);
         if (n <= 1 || g0 + (int)(threadIdx.x & 63) >= g) n = 0;
-        slot += __shfl(wave_prefix(n), 63);
+        slot += __builtin_amdgcn_readlane(wave_prefix(n), 63);
     }
     const int ranges = tiles_of(offsets, G, total, height, g, lo, len);
-    if (ranges == 1) return;
+    if (ranges == 1 || (ranges > 1 && slot + ranges > slots)) return;  // (the second: offsets that are none)
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < per_group; i += (int64_t)gridDim.x * 1024) {
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         const float* p = partial + (int64_t)slot * per_group + i;
-        for (int k = 0; k < ranges; ++k) sum += *(const f32x4*)(p + (int64_t)k * per_group);
+        for (int k = 0; k < ranges; k += SLOT_FETCH) {
+            f32x4 x[SLOT_FETCH];
+#pragma unroll
+            for (int u = 0; u < SLOT_FETCH; ++u) x[u] = __builtin_nontemporal_load((const f32x4*)(p + (int64_t)(k + u < ranges ? k + u : k) * per_group));
+#pragma unroll
+            for (int u = 0; u < SLOT_FETCH; ++u)
+                if (k + u < ranges) sum += x[u];
+        }
         typedef __attribute__((ext_vector_type(4))) T T4;
         T4 o;
 #pragma unroll
@@ -251,7 +261,7 @@ WeightsPlan plan_weights(int G, int64_t total, int K, int N, int dtype) {
         for (int r = 1; r <= 4; ++r)  // whole rounds
             if (const double ranges = r * resident / tiles - more; ranges >= 1) consider(total / ranges);
     }
-    best.slots = 2 * total / best.height;  // (a group with a slot has more than one range, so more rows than one)
+    best.slots = best.height < total ? 2 * total / best.height : 0;  // (a group with a slot has more than one range, so more rows than one)
     return best;
 }
 template <typename S, typename T>
@@ -259,7 +269,7 @@ void weights_of(const WeightsPlan& p, const void* x, const void* dy, void* dw, f
                 int N, hipStream_t stream) {
     const int n_tiles = (N + S::BN - 1) / S::BN, k_tiles = (K + S::BM - 1) / S::BM;
     hipLaunchKernelGGL((grouped_weights_kernel<S, T>), tile_grid(row_tiles(G, total, p.height) * k_tiles * n_tiles, S::THREADS), dim3(S::THREADS), 0, stream, (const T*)x, (const T*)dy, (T*)dw,
-                       partial, offsets, G, total, K, N, p.height, n_tiles,
+                       partial, offsets, G, total, K, N, p.height, p.slots, n_tiles,
                        k_tiles < BAND ? k_tiles : BAND);
 }
 template <typename T>
@@ -275,7 +285,7 @@ void weights(const void* x, const void* dy, void* dw, const int32_t* offsets, in
     }
     const int64_t per_group = (int64_t)K * N, blocks = (per_group + 1023) / 1024;
     hipLaunchKernelGGL(grouped_join_kernel<T>, dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)G), dim3(256), 0, stream, partial, (T*)dw,
-                       offsets, G, total, per_group, p.height);
+                       offsets, G, total, per_group, p.height, p.slots);
 }
 
 }  // namespace

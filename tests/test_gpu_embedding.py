@@ -138,3 +138,32 @@ def test_many_rows_of_one_value(kb):
     assert bool((g[0] == 3).all()) and bool((g[1] == 3).all()) and not g[2].any()
     out = kb.embedding_fwd(g, ids)
     assert bool((out == 3).all())
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("D", [8, 203, 256])
+def test_tensors_that_start_anywhere(kb, D, dtype):
+    """Views that begin one value into their memory: rows at any multiple of the value's size."""
+    view = lambda n, seed: R.normal((n * D + 1,), dtype, seed)[1:].view(n, D)
+    table, d_out, ids = view(40, 1), view(90, 2), make_ids("skewed", 91, 40, 3, torch.int32)[1:]
+    out, grad = view(90, 4), view(40, 5)
+    kb.embedding_fwd(table, ids, 3.0, out=out)
+    kb.embedding_bwd(d_out, ids, 40, 3.0, out=grad)
+    R.check("out", out, *R.embedding_fwd(table, ids, 3.0), dtype)
+    R.check("d_table", grad, *R.embedding_bwd(d_out, ids, 40, 3.0), dtype)
+
+
+@pytest.mark.parametrize("V,D", [(270_000, 513), (1_100_000, 128)])
+def test_tables_that_are_not_set_to_zero_first(kb, V, D):
+    """Gradients above 256 MB: rows without ids are found among the sorted ids."""
+    n, dtype = 6000, torch.bfloat16
+    ids = make_ids("each", n, V, 1, torch.int64)
+    ids[::7], ids[5::11] = V - 1, -1
+    d_out = R.normal((n, D), dtype, 2)
+    got = kb.embedding_bwd(d_out, ids, V, 1.0, out=torch.full((V, D), float("nan"), dtype=dtype, device="cuda"))
+    named = torch.unique(ids[ids >= 0])
+    small = torch.searchsorted(named, ids)
+    small[ids < 0] = -1
+    R.check("d_table", got[named], *R.embedding_bwd(d_out, small, len(named), 1.0), dtype)
+    got[named] = 0
+    assert not bool(got.any())

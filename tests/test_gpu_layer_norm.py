@@ -110,3 +110,17 @@ def test_rows_beyond_32_bit_offsets(kb):
     assert torch.equal(dx[some], small[0])
     dx[some] = 0
     assert not bool(dx.any())
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("D", [9, 256, 4097])
+def test_tensors_that_start_anywhere(kb, D, dtype):
+    """Views that begin one value into their memory: rows at any multiple of the value's size."""
+    view = lambda n, seed: R.normal((n * D + 1,), dtype, seed)[1:].view(n, D)
+    x, dy, w, b = view(13, 1), view(13, 2), view(1, 3)[0], view(1, 4)[0]
+    y, mean, rstd = kb.layer_norm_fwd(x, w, b, EPS, out=view(13, 5))
+    (ref, bound), *_ = R.norm_fwd(x, w, b, EPS)
+    R.check("y", y, ref, bound, dtype)
+    outs = view(13, 6), view(1, 7)[0], view(1, 8)[0]
+    for name, t, (ref, bound) in zip(("dx", "dw", "db"), kb.layer_norm_bwd(x, w, dy, mean, rstd, out=outs), R.norm_bwd(x, w, dy, mean, rstd)):
+        R.check(name, t, ref, bound, dtype)
