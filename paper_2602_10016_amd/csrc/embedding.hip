@@ -328,6 +328,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const ID* __re
 
 constexpr int ADD_FETCH = 8;  // rows in flight per lane group
 constexpr int JOIN_FETCH = 8, JOIN_ALONE = 16;  // partial sums in flight; ranges of a run that one lane group adds
+constexpr int JOIN_STARTS = 16;                 // ranges per workgroup: few runs that begin in them are long
 constexpr int JOIN_SUMS = 16;                   // most parts of a longer one that are added one after another
 constexpr int ZERO_ROWS = 64; // table rows that a workgroup searches for
 
@@ -441,16 +442,17 @@ template <typename T, int W>
 __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t* __restrict__ keys, const float* __restrict__ partial,
                                                                  T* __restrict__ d_table, int64_t n, uint32_t rows, int D, float scale, int lanes,
                                                                  int64_t chunk) {
-    __shared__ int64_t last_of[THREADS];     // of the run that begins in a lane group's range: the last range it is in (0: none to add)
-    __shared__ uint32_t key_of[THREADS];
+    __shared__ int64_t last_of[JOIN_STARTS];  // of the run that begins in a lane group's range: the last range it is in (0: none to add)
+    __shared__ uint32_t key_of[JOIN_STARTS];
     __shared__ float parts[THREADS * W];     // [groups][lanes][W]
     const int pieces = (D + W - 1) / W;
     const int lane = threadIdx.x % lanes, c = blockIdx.y * 64 + lane, group = threadIdx.x / lanes, groups = THREADS / lanes;
     const bool has = c < pieces;
-    const int64_t walker0 = (int64_t)blockIdx.x * groups, walker = walker0 + group, i0 = walker * chunk, i1 = i0 + chunk;
+    const int starts = groups < JOIN_STARTS ? groups : JOIN_STARTS;  // ranges that the workgroup looks at
+    const int64_t walker0 = (int64_t)blockIdx.x * starts, walker = walker0 + group, i0 = walker * chunk, i1 = i0 + chunk;
     int64_t last = 0;
     uint32_t key = 0;
-    if (i1 < n) {
+    if (group < starts && i1 < n) {
         key = keys[i1 - 1];
         if (key < rows && keys[i1] == key && !(i0 > 0 && keys[i0 - 1] == key)) {
             // the range that holds the run's last pair; most runs end in the next one
@@ -473,12 +475,12 @@ __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t*
         add_ranges<W>(acc, partial, walker + 1, last + 1, pieces, cc);
         finish(acc, key);
     }
-    if (lane == 0) {
+    if (lane == 0 && group < starts) {
         last_of[group] = together ? last : 0;
         key_of[group] = key;
     }
     __syncthreads();
-    for (int w = 0; w < groups; ++w) {
+    for (int w = 0; w < starts; ++w) {
         const int64_t end = last_of[w] + 1;
         if (end == 1) continue;
         const int64_t first = walker0 + w + 1, per = (end - first + groups - 1) / groups, mine = first + group * per;
@@ -621,8 +623,9 @@ void embedding_bwd(const void* d_out, const SortSpace& s, void* d_table, int64_t
     const unsigned tiles = (unsigned)((pieces + 63) / 64);
     hipLaunchKernelGGL((embedding_add_kernel<T, W>), dim3((unsigned)(add_blocks + zero_blocks), tiles), dim3(THREADS), 0, stream, (const T*)d_out,
                        s.keys, s.positions, (T*)d_table, s.partial, n, (uint32_t)rows, D, scale, lanes, chunk, add_blocks);
+    const int starts = groups < JOIN_STARTS ? groups : JOIN_STARTS;
     if (ranges > 1)
-        hipLaunchKernelGGL((embedding_join_kernel<T, W>), dim3((unsigned)add_blocks, tiles), dim3(THREADS), 0, stream, s.keys, s.partial,
+        hipLaunchKernelGGL((embedding_join_kernel<T, W>), dim3((unsigned)((ranges + starts - 1) / starts), tiles), dim3(THREADS), 0, stream, s.keys, s.partial,
                            (T*)d_table, n, (uint32_t)rows, D, scale, lanes, chunk);
 }
 

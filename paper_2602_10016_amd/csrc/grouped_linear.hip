@@ -122,6 +122,78 @@ __global__ __launch_bounds__(S::THREADS, 2) void grouped_rows_kernel(const T* __
     grouped_store<S, T>(acc, lds, out + t.row0 * N + n0, N, t.rows, N - n0, lane, wave);
 }
 
+// The same for few rows and long contractions: 32 x 32 outputs per workgroup, whose eight waves take an eighth of the contraction each, through
+// rings of their own (no barriers), and add up in order.  Five rows of 3416 values, 464 columns, fp32: 18 us (70 by Small tiles); bound by the latency of a wave's steps.
+constexpr int DEEP = 32, DEEP_WAVES = 8;
+template <typename T, bool B_COLUMNS>
+__global__ __launch_bounds__(64 * DEEP_WAVES, 2) void grouped_rows_deep_kernel(const T* __restrict__ in, const T* __restrict__ w, T* __restrict__ out,
+                                                                               const int32_t* __restrict__ offsets, int G, int64_t total, int K,
+                                                                               int N, bool fill_rest, int n_tiles, int band) {
+    using S = GroupedShape<DEEP, DEEP, 1, 1, 2>;  // of one wave
+    __shared__ __attribute__((aligned(1024))) char lds[DEEP_WAVES * 2 * S::STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t mt;
+    int nt;
+    if (!tile_of(count_row_tiles(offsets, G, total, DEEP, fill_rest), n_tiles, band, 32, mt, nt)) return;
+    constexpr uint32_t E = sizeof(T);
+    const RowTile t = find_row_tile<false>(offsets, G, total, DEEP, mt);
+    const int n0 = nt * DEEP;
+    f32x16 acc[1][1] = {};
+    char* const mine = lds + wave * (2 * S::STAGE);
+    if (t.group < G) {
+        const T* wg = w + (int64_t)t.group * K * N;
+        GroupedDma<T, DEEP, 1, S::STEP_BYTES, false> dma_a;
+        GroupedDma<T, DEEP, 1, S::STEP_BYTES, B_COLUMNS> dma_b;
+        dma_a.init({(const char*)(in + t.row0 * K), (uint32_t)K * E, t.rows}, lane, 0);
+        dma_b.init({(const char*)(B_COLUMNS ? wg + n0 : wg + (int64_t)n0 * K), (uint32_t)(B_COLUMNS ? N : K) * E, N - n0}, lane, 0);
+        GroupedFrag<T, DEEP, S::STEP_BYTES, false> frag_a;
+        GroupedFrag<T, DEEP, S::STEP_BYTES, B_COLUMNS> frag_b;
+        frag_a.init(lane, 0);
+        frag_b.init(lane, 0);
+        constexpr int STEP = decltype(dma_a)::STEP, LOADS = decltype(dma_a)::LOADS + decltype(dma_b)::LOADS;
+        const int steps = (K + STEP - 1) / STEP, per = (steps + DEEP_WAVES - 1) / DEEP_WAVES;
+        const int k0 = wave * per, k1 = k0 + per < steps ? k0 + per : steps;
+        const uint32_t lds0 = lds_address(mine);
+        auto issue = [&](int k) {
+            const uint32_t stage = lds0 + (k & 1) * S::STAGE;
+            dma_a.issue(k, K - k * STEP, stage);
+            dma_b.issue(k, K - k * STEP, stage + S::A_BYTES);
+        };
+        if (k0 < k1) issue(k0);
+        for (int k = k0; k < k1; ++k) {
+            wait_lds();  // the reads of the step before: its stage is loaded next
+            if (k + 1 < k1) {
+                issue(k + 1);
+                wait_vmcnt<LOADS>();
+            } else {
+                wait_vmcnt<0>();
+            }
+            asm volatile("" ::: "memory");  // (the step is read behind the wait)
+            const char* ta = mine + (k & 1) * S::STAGE;
+            grouped_step<S, T>(acc, ta, ta + S::A_BYTES, frag_a, frag_b);
+        }
+        wait_lds();
+    }
+    // a wave's sums as rows of 33 floats in its own ring; then two outputs per thread
+    float* const sums = (float*)mine;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sums[(lane & 31) * 33 + c_row(v, lane >> 5)] = acc[0][0][v];
+    __syncthreads();
+    const int m = threadIdx.x / 16, n = threadIdx.x % 16 * 2;
+    float total_0 = 0.f, total_1 = 0.f;
+#pragma unroll
+    for (int q = 0; q < DEEP_WAVES; ++q) {
+        const float* const p = (const float*)(lds + q * (2 * S::STAGE)) + m * 33 + n;
+        total_0 += p[0];
+        total_1 += p[1];
+    }
+    if (m < t.rows && n0 + n < N) {
+        T* const o = out + (t.row0 + m) * N + n0 + n;
+        o[0] = from_float<T>(total_0);
+        o[1] = from_float<T>(total_1);
+    }
+}
+
 // dw[g] = x^T dy over a range of `height` rows of group g, to dw where the group has no other range, else to the range's slot of `partial`.
 template <typename S, typename T>
 __global__ __launch_bounds__(S::THREADS) void grouped_weights_kernel(const T* __restrict__ x, const T* __restrict__ dy, T* __restrict__ dw,
@@ -195,9 +267,28 @@ void rows_of(const void* in, const void* w, void* out, const int32_t* offsets, i
     hipLaunchKernelGGL((grouped_rows_kernel<S, T, B_COLUMNS>), tile_grid(row_tiles(G, total, S::BM) * n_tiles, S::THREADS), dim3(S::THREADS), 0, stream, (const T*)in, (const T*)w,
                        (T*)out, offsets, G, total, K, N, fill_rest, n_tiles, BAND);
 }
-// Tiles of a launch that have rows, about: every group that can have any ends half a tile early.
+template <typename T, bool B_COLUMNS>
+void rows_deep(const void* in, const void* w, void* out, const int32_t* offsets, int G, int64_t total, int K, int N, bool fill_rest,
+               hipStream_t stream) {
+    const int n_tiles = (N + DEEP - 1) / DEEP;
+    hipLaunchKernelGGL((grouped_rows_deep_kernel<T, B_COLUMNS>), tile_grid(row_tiles(G, total, DEEP) * n_tiles, 64 * DEEP_WAVES),
+                       dim3(64 * DEEP_WAVES), 0, stream, (const T*)in, (const T*)w, (T*)out, offsets, G, total, K, N, fill_rest, n_tiles, BAND);
+}
+
+// Tiles of a launch that have rows, about: one per group where groups are smaller than a tile, else every group ends half a tile early.
 int64_t tiles_with_rows(int G, int64_t total, int columns, int height, int width) {
-    return (total / height + (G < total ? G : total) / 2 + 1) * ((columns + width - 1) / width);
+    const int64_t groups = G < total ? G : total;
+    return (total < groups * height ? groups : total / height + groups / 2) * ((columns + width - 1) / width);
+}
+// Whether 32 x 32 tiles of eight waves over the contraction are faster than Small ones of four over the outputs: us of their rounds (a round
+// holds one Deep or three Small workgroups per compute unit) as measured; Small waits for each of its steps, Deep for an eighth of them.
+// bf16: 5 rows, 3416 -> 464: 7.6 / 18.8 us, 64 rows, 4096 -> 4096: 13.5 / 22.0, 61 rows in 3 groups, 1264 -> 3728: 12.0 / 10.2; fp32: 18 / 70,
+// 24 / 86, 20 / 30.
+bool deep_pays(int G, int64_t total, int K, int N, int elt) {
+    const int64_t steps = ((int64_t)K * elt + 127) / 128, cu = compute_units();
+    const double deep = (double)((tiles_with_rows(G, total, N, DEEP, DEEP) + cu - 1) / cu) * (4 + 0.14 * steps);
+    const double small = (double)((tiles_with_rows(G, total, N, 64, 64) + 3 * cu - 1) / (3 * cu)) * (3 + (elt == 4 ? 0.66 : 0.33) * steps);
+    return deep < small;
 }
 
 // The largest tile of which there are enough to fill the device.  A Large tile moves least through LDS (262 144 rows, 1024 -> 4096: 1000
@@ -219,6 +310,8 @@ void rows(const void* in, const void* w, void* out, const int32_t* offsets, int 
         }
     if (tiles_with_rows(G, total, N, 128, 128) >= (sizeof(T) == 2 && B_COLUMNS ? cu : 2 * cu))
         rows_of<Middle, T, B_COLUMNS>(in, w, out, offsets, G, total, K, N, fill_rest, stream);
+    else if (deep_pays(G, total, K, N, sizeof(T)))
+        rows_deep<T, B_COLUMNS>(in, w, out, offsets, G, total, K, N, fill_rest, stream);
     else
         rows_of<Small, T, B_COLUMNS>(in, w, out, offsets, G, total, K, N, fill_rest, stream);
 }

@@ -5,7 +5,7 @@
 // form; nothing is transposed in memory.  Steps of 64 contraction values travel straight from memory into a ring of LDS stages
 // (buffer loads to LDS); fragments of a row-form tile are 16-byte reads, of a column-form tile transposing reads (mfma_tile.h).
 //   LDS, row form:     128 bytes per row, 16-byte chunk ^= (row / 2) % 8: 16 consecutive rows of one chunk hit 16 different places
-//   LDS, column form:  2 W bytes per contraction row, 64-byte group ^= row % 4 (W = 64: (row / 2) % 2): four rows of one group, likewise
+//   LDS, column form:  2 W bytes per contraction row, 64-byte group ^= row % 4 (W = 64: (row / 2) % 2, W = 32: nothing): four rows of one group, likewise
 // What lies outside is handled where it is loaded: rows and columns of C outside the tile re-read the last valid one (never stored);
 // contraction values outside are zeros in both operands (a buffer load outside its descriptor's range gives zero), so that an infinity next
 // to them does no harm.
@@ -15,6 +15,9 @@
 #include "lds_ring.h"
 
 namespace kunlun {
+
+// s_waitcnt that waits for LDS operations only.
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4)); }
 
 constexpr uint32_t GL_OUTSIDE = 0x80000000u;     // an offset outside every descriptor
 
@@ -40,7 +43,7 @@ struct GroupedDma {
 
     __device__ static __forceinline__ int swizzle(int row) {
         if (!COLUMNS) return STEP_BYTES == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
-        return E == 4 ? 0 : ROW_BYTES >= 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+        return E == 4 || ROW_BYTES == 64 ? 0 : ROW_BYTES >= 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
     }
     __device__ __forceinline__ int row_of(int i) const { return (wave_ * LOADS + i) * ROWS + lane_ / CHUNKS; }
     __device__ __forceinline__ int chunk_of(int i) const { return (lane_ % CHUNKS) ^ swizzle(row_of(i)); }
@@ -93,7 +96,7 @@ struct GroupedFrag {
             const int s16 = lane & 15, hi16 = (lane >> 4) & 1;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int row = 8 * g + 4 * half + (s16 >> 2), x = ROW_BYTES >= 256 ? row & 3 : (row >> 1) & 1;
+                const int row = 8 * g + 4 * half + (s16 >> 2), x = ROW_BYTES >= 256 ? row & 3 : ROW_BYTES == 128 ? (row >> 1) & 1 : 0;
                 at[half] = row * ROW_BYTES + (((first / 32) ^ x) << 6) + (16 * hi16 + 4 * (s16 & 3)) * 2;
             }
         } else if constexpr (COLUMNS) {
