@@ -454,9 +454,15 @@ __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t*
     uint32_t key = 0;
     if (group < starts && i1 < n) {
         key = keys[i1 - 1];
-        if (key < rows && keys[i1] == key && !(i0 > 0 && keys[i0 - 1] == key)) {
-            // the range that holds the run's last pair; most runs end in the next one
-            last = i1 + chunk >= n || keys[i1 + chunk] != key ? walker + 1 : (first_at_least(keys, i1 + chunk, n, key + 1) - 1) / chunk;
+        const uint32_t behind = keys[i1], before = keys[i0 > 0 ? i0 - 1 : 0], further = keys[i1 + chunk < n ? i1 + chunk : n - 1];
+        if (key < rows && behind == key && !(i0 > 0 && before == key)) {
+            // the range that holds the run's last pair: most end in the next one, the others are searched for in growing steps
+            last = walker + 1;
+            if (i1 + chunk < n && further == key) {
+                int64_t at = i1 + chunk, step = 2 * chunk;
+                for (; at + step < n && keys[at + step] == key; step *= 2) at += step;
+                last = (first_at_least(keys, at + 1, at + step < n ? at + step : n, key + 1) - 1) / chunk;
+            }
         }
     }
     auto finish = [&](const float (&acc)[W], uint32_t k) {
@@ -543,7 +549,7 @@ void embedding_fwd(const void* table, const void* ids, void* out, int64_t n, int
 // Pairs per lane group: ranges enough to fill the device (16 waves per compute unit of them), long ones otherwise, so that few runs
 // cross a range and leave partial sums (1.1 million rows of 64, eight lanes each: 119 us with 8942 ranges, 109 us with 35 769).
 constexpr int64_t CHUNK_LEAST = 8;
-int64_t ranges_most(int lanes) { return lanes < 32 ? ((int64_t)1 << 19) / lanes : 1 << 14; }
+int64_t ranges_most(int lanes) { return lanes < 8 ? 1 << 16 : lanes < 32 ? (1 << 19) / lanes : 1 << 14; }
 int64_t add_chunk(int64_t n, int lanes) {
     int64_t chunk = CHUNK_LEAST;
     while ((n + chunk - 1) / chunk > ranges_most(lanes)) chunk *= 2;
