@@ -2,6 +2,11 @@
 // Groups have any sizes, so the work is cut into output tiles and a workgroup finds its tile from the offsets: tiles of rows are
 // counted per group (a launch has room for the tiles of any division of the rows, those left over end at once).
 // The products run on the matrix cores (grouped_tile.h).
+// Measured, bf16 (a large product of the library reaches 1110 TFLOP/s here, under the power limit): 262 144 rows in 16 groups, 1024 -> 4096,
+// forward 2.14 ms (1030 TFLOP/s), gradient of the rows 2.02 (1090), of the weights 2.2 to 2.4 (920 to 1000); 139 264 rows in 8 groups, 256 -> 768:
+// 85, 65 and 79 us, where 56 are the bytes of each.  One row in each of 16 groups, 4096 -> 4096: 76 us = 7.0 TB/s of weights.  fp32: 30 000
+// rows, 2048 -> 2048, 1.8 ms (140 TFLOP/s of 154).  The matrix units are busy for 58 % of the cycles of a long product, at 1.65 GHz; other
+// orders of the loads and reads of a step, priorities and tiles of four waves moved nothing by more than the clock does.
 #include <cmath>
 
 #include "grouped_tile.h"
