@@ -6,7 +6,8 @@
 // The gradient sorts (id, position) pairs with a stable radix sort, then lane groups walk fixed ranges of the sorted pairs and
 // add the rows of equal ids in registers: no float atomics, so equal calls give equal bits, and a row of d_out is read once
 // wherever it lies.  A run of equal ids inside one range is written to its table row at once; a run that crosses ranges leaves
-// one fp32 partial sum per range, which a second kernel adds in order (an id may be in a large part of the rows).  Small tables are set
+// one fp32 partial sum per range (or one for all ranges of a workgroup that are inside it), which a second kernel adds in order: an id may
+// be in a large part of the rows.  Small tables are set
 // to zero beside the sort; in larger ones the rows that no id names are found among the sorted ids, so that they are written once.
 // Measured (bf16; a copy reaches 5.07 TB/s here): lookup of 139 264 rows of 256 21 us (5.6 TB/s, repeated rows come from the caches);
 // gradient of 1 144 603 rows of 1024 into a million 942 us (4.7 TB/s), of which the sums are 870, sorting 58 in six
@@ -348,8 +349,8 @@ __device__ __forceinline__ int64_t first_at_least(const uint32_t* keys, int64_t 
 template <typename T, int W>
 __global__ __launch_bounds__(THREADS) void embedding_add_kernel(const T* __restrict__ d_out, const uint32_t* __restrict__ keys,
                                                                 const uint32_t* __restrict__ positions, T* __restrict__ d_table,
-                                                                float* __restrict__ partial, int64_t n, uint32_t rows, int D, float scale, int lanes,
-                                                                int64_t chunk, int64_t add_blocks) {
+                                                                float* __restrict__ partial, float* __restrict__ whole, int64_t n, uint32_t rows,
+                                                                int D, float scale, int lanes, int64_t chunk, int64_t add_blocks) {
     const int pieces = (D + W - 1) / W;
     const int c = blockIdx.y * 64 + threadIdx.x % lanes;
     const bool has = c < pieces;
@@ -379,10 +380,36 @@ __global__ __launch_bounds__(THREADS) void embedding_add_kernel(const T* __restr
     }
     const int64_t walker = blockIdx.x * groups + group;
     const int64_t i0 = walker * chunk, i1 = i0 + chunk < n ? i0 + chunk : n;
-    if (i0 >= n || !has) return;
     float acc[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) acc[j] = 0.f;
+    // all ranges of the workgroup inside one run: one partial sum for them
+    const int64_t b0 = (int64_t)blockIdx.x * groups * chunk, b1 = b0 + groups * chunk;
+    if (b0 > 0 && b1 < n && keys[b0 - 1] == keys[b1]) {
+        if (keys[b1] >= rows) return;
+        __shared__ float parts[THREADS * W];
+        for (int64_t i = i0; i < i1; i += ADD_FETCH) {
+            Piece<T, W> x[ADD_FETCH];
+#pragma unroll
+            for (int u = 0; u < ADD_FETCH; ++u) x[u] = load_piece<T, W>(d_out + (int64_t)positions[i + u] * D + at);
+#pragma unroll
+            for (int u = 0; u < ADD_FETCH; ++u)
+#pragma unroll
+                for (int j = 0; j < W; ++j) acc[j] += to_float(x[u].v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) parts[threadIdx.x * W + j] = acc[j];
+        __syncthreads();
+        if (group > 0 || !has) return;
+        for (int g = 1; g < groups; ++g)
+#pragma unroll
+            for (int j = 0; j < W; ++j) acc[j] += parts[(g * lanes + threadIdx.x) * W + j];
+        float* const p = whole + ((int64_t)blockIdx.x * pieces + c) * W;
+#pragma unroll
+        for (int j = 0; j < W; ++j) p[j] = acc[j];
+        return;
+    }
+    if (i0 >= n || !has) return;
     uint32_t key = keys[i0];
     bool from_before = i0 > 0 && keys[i0 - 1] == key;
     auto finish = [&](bool goes_on) {
@@ -424,14 +451,40 @@ __global__ __launch_bounds__(THREADS) void embedding_add_kernel(const T* __restr
     finish(i1 < n && keys[i1] == key);
 }
 
-// acc += the partial sums in slot 0 of the ranges begin .. end - 1, in order
+// The partial sums of a run behind the range where it begins, in order: of ranges (slot 0) up to the first workgroup of the kernel above
+// whose ranges are all inside the run, of those workgroups, of the ranges behind them.
+struct RunSums {
+    const float *partial, *whole;
+    int64_t first, lead, blocks, block0, tail0, count;  // the first range; how many ranges and workgroups; the first workgroup; the range behind
+    __device__ __forceinline__ RunSums(const float* partial_, const float* whole_, int64_t walker, int64_t last, int per_block)
+        : partial(partial_), whole(whole_), first(walker + 1) {
+        block0 = (walker + per_block) / per_block;
+        blocks = last / per_block - block0;
+        if (blocks <= 0) {
+            blocks = 0;
+            lead = last - walker;
+            tail0 = last + 1;
+        } else {
+            lead = block0 * per_block - first;
+            tail0 = (block0 + blocks) * per_block;
+        }
+        count = lead + blocks + (last + 1 - tail0);
+    }
+    __device__ __forceinline__ const float* at(int64_t i, int pieces, int c, int W) const {
+        if (i < lead) return partial + ((first + i) * 2 * pieces + c) * W;
+        i -= lead;
+        if (i < blocks) return whole + ((block0 + i) * pieces + c) * W;
+        return partial + ((tail0 + i - blocks) * 2 * pieces + c) * W;
+    }
+};
+// acc += sums begin .. end - 1
 template <int W>
-__device__ __forceinline__ void add_ranges(float (&acc)[W], const float* partial, int64_t begin, int64_t end, int pieces, int c) {
+__device__ __forceinline__ void add_sums(float (&acc)[W], const RunSums& sums, int64_t begin, int64_t end, int pieces, int c) {
     for (int64_t r = begin; r < end; r += JOIN_FETCH) {
         float x[JOIN_FETCH][W];
 #pragma unroll
         for (int u = 0; u < JOIN_FETCH; ++u)
-            __builtin_memcpy(x[u], __builtin_assume_aligned(partial + ((r + u < end ? r + u : begin) * 2 * pieces + c) * W, W % 4 ? 4 : 16), sizeof(x[u]));
+            __builtin_memcpy(x[u], __builtin_assume_aligned(sums.at(r + u < end ? r + u : begin, pieces, c, W), W % 4 ? 4 : 16), sizeof(x[u]));
 #pragma unroll
         for (int u = 0; u < JOIN_FETCH; ++u)
 #pragma unroll
@@ -439,10 +492,11 @@ __device__ __forceinline__ void add_ranges(float (&acc)[W], const float* partial
     }
 }
 
-// Runs that cross ranges.  The lane group of the range where one begins adds its partial sums in order; a run over more than JOIN_ALONE
-// ranges is shared by the lane groups of the workgroup, each of which adds a part, and the parts are added in order.
+// Runs that cross ranges.  The lane group of the range where one begins adds its partial sums in order; a run of more than JOIN_ALONE
+// sums is shared by the lane groups of the workgroup, each of which adds a part, and the parts are added in order.
 template <typename T, int W>
 __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t* __restrict__ keys, const float* __restrict__ partial,
+                                                                 const float* __restrict__ whole,
                                                                  T* __restrict__ d_table, int64_t n, uint32_t rows, int D, float scale, int lanes,
                                                                  int64_t chunk) {
     __shared__ int64_t last_of[JOIN_STARTS];  // of the run that begins in a lane group's range: the last range it is in (0: none to add)
@@ -475,13 +529,14 @@ __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t*
         if (has) store_piece<T, W>(d_table + (int64_t)k * D + piece_start(c, D, W), y);
     };
     const int cc = has ? c : pieces - 1;
-    const bool together = last - walker > JOIN_ALONE;
+    const RunSums mine_sums(partial, whole, walker, last ? last : walker, groups);
+    const bool together = mine_sums.count > JOIN_ALONE;
     if (last && !together) {
         float acc[W];
         const float* p = partial + ((walker * 2 + 1) * pieces + cc) * W;
 #pragma unroll
         for (int j = 0; j < W; ++j) acc[j] = p[j];
-        add_ranges<W>(acc, partial, walker + 1, last + 1, pieces, cc);
+        add_sums<W>(acc, mine_sums, 0, mine_sums.count, pieces, cc);
         finish(acc, key);
     }
     if (lane == 0 && group < starts) {
@@ -490,9 +545,9 @@ __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t*
     }
     __syncthreads();
     for (int w = 0; w < starts; ++w) {
-        const int64_t end = last_of[w] + 1;
-        if (end == 1) continue;
-        const int64_t first = walker0 + w + 1, per = (end - first + groups - 1) / groups, mine = first + group * per;
+        if (last_of[w] == 0) continue;
+        const RunSums sums(partial, whole, walker0 + w, last_of[w], groups);
+        const int64_t per = (sums.count + groups - 1) / groups, mine = group * per;
         float acc[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) acc[j] = 0.f;
@@ -501,7 +556,7 @@ __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t*
 #pragma unroll
             for (int j = 0; j < W; ++j) acc[j] = p[j];
         }
-        add_ranges<W>(acc, partial, mine, mine + per < end ? mine + per : end, pieces, cc);
+        add_sums<W>(acc, sums, mine, mine + per < sums.count ? mine + per : sums.count, pieces, cc);
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < W; ++j) parts[threadIdx.x * W + j] = acc[j];
@@ -511,22 +566,22 @@ __global__ __launch_bounds__(THREADS) void embedding_join_kernel(const uint32_t*
 #pragma unroll
                 for (int j = 0; j < W; ++j) acc[j] += parts[(g * lanes + lane) * W + j];
         };
-        const int sums = groups < JOIN_SUMS ? groups : JOIN_SUMS, span = groups / sums;
+        const int joined = groups < JOIN_SUMS ? groups : JOIN_SUMS, span = groups / joined;
         if (span > 1) {  // (many narrow lane groups: their parts in two steps)
             const int g0 = group * span;
-            if (group < sums) {
+            if (group < joined) {
 #pragma unroll
                 for (int j = 0; j < W; ++j) acc[j] = 0.f;
                 add_parts(g0, g0 + span);
             }
             __syncthreads();
-            if (group < sums)
+            if (group < joined)
 #pragma unroll
                 for (int j = 0; j < W; ++j) parts[threadIdx.x * W + j] = acc[j];
             __syncthreads();
         }
         if (group == 0) {
-            add_parts(1, sums);
+            add_parts(1, joined);
             finish(acc, key_of[w]);
         }
     }
@@ -567,7 +622,7 @@ struct SortSpace {
     uint2* pairs[2];
     uint32_t *keys, *positions;  // in the end
     uint32_t *counts, *totals;
-    float* partial;
+    float *partial, *whole;  // per range, per workgroup of ranges
     size_t bytes;
     SortSpace(char* base, int64_t n, int D, int dtype) {
         size_t at = 0;
@@ -580,7 +635,10 @@ struct SortSpace {
         totals = (uint32_t*)take(BINS_MOST * 4);
         const int W = dtype == KUNLUN_FP32 ? piece_width<float>(D) : piece_width<bf16_t>(D);
         const int pieces = pieces_per_row(D, W);
-        partial = (float*)take((size_t)ranges_at_most(n, lanes_per_row(pieces)) * 2 * pieces * W * 4);
+        const int lanes = lanes_per_row(pieces);
+        const int64_t ranges = ranges_at_most(n, lanes);
+        partial = (float*)take((size_t)ranges * 2 * pieces * W * 4);
+        whole = (float*)take((size_t)(ranges / (THREADS / lanes) + 1) * pieces * W * 4);
         bytes = at;
     }
 };
@@ -631,10 +689,11 @@ void embedding_bwd(const void* d_out, const SortSpace& s, void* d_table, int64_t
     const int64_t zero_blocks = filled ? 0 : zero_all < GRID_MOST ? zero_all : GRID_MOST;
     const unsigned tiles = (unsigned)((pieces + 63) / 64);
     hipLaunchKernelGGL((embedding_add_kernel<T, W>), dim3((unsigned)(add_blocks + zero_blocks), tiles), dim3(THREADS), 0, stream, (const T*)d_out,
-                       s.keys, s.positions, (T*)d_table, s.partial, n, (uint32_t)rows, D, scale, lanes, chunk, add_blocks);
+                       s.keys, s.positions, (T*)d_table, s.partial, s.whole, n, (uint32_t)rows, D, scale, lanes, chunk,
+                       add_blocks);
     const int starts = groups < JOIN_STARTS ? groups : JOIN_STARTS;
     if (ranges > 1)
-        hipLaunchKernelGGL((embedding_join_kernel<T, W>), dim3((unsigned)((ranges + starts - 1) / starts), tiles), dim3(THREADS), 0, stream, s.keys, s.partial,
+        hipLaunchKernelGGL((embedding_join_kernel<T, W>), dim3((unsigned)((ranges + starts - 1) / starts), tiles), dim3(THREADS), 0, stream, s.keys, s.partial, s.whole,
                            (T*)d_table, n, (uint32_t)rows, D, scale, lanes, chunk);
 }
 
