@@ -10,9 +10,8 @@
 // be in a large part of the rows.  Small tables are set
 // to zero beside the sort; in larger ones the rows that no id names are found among the sorted ids, so that they are written once.
 // Measured (bf16; a copy reaches 5.07 TB/s here): lookup of 139 264 rows of 256 21 us (5.6 TB/s, repeated rows come from the caches);
-// gradient of 1 144 603 rows of 1024 into a million 942 us (4.7 TB/s), of which the sums are 870, sorting 58 in six
-// launches and joining 23; of 139 264 rows of 256 into
-// 200 000 79 us: sort 40 in four launches of 5 and 15 us that leave most compute units idle, sums 24, joining 13.
+// gradient of 1 144 603 rows of 1024 into a million 934 us (4.7 TB/s), of which the sums are 870, sorting 60 in six launches and joining 22;
+// of 139 264 rows of 256 into 200 000 75 us: sorting 42 in four launches that leave most compute units idle, sums 23, joining 9.
 #include "layers.h"
 
 namespace kunlun {

@@ -8,7 +8,7 @@
 // keeps its columns' sums in registers, joins its lane groups through LDS in order and leaves one fp32 row per workgroup; a
 // second kernel adds those in order.  No atomics: equal calls give equal bits.
 // Measured (a copy reaches 5.07 TB/s here): forward of 139 264 bf16 rows of 256 29 us (4.9 TB/s); backward of 1 144 603 rows of 1024
-// 1.26 ms (5.6 TB/s, two reads to a write); of 9973 fp32 rows of 203 13.0 us, 8 of them the rows', 4 the column sums'.  A vector
+// 1.27 ms (5.5 TB/s, two reads to a write); of 9973 fp32 rows of 203 13.0 us, 8.6 of them the rows', 4 the column sums'.  A vector
 // operation per step instead of an LDS exchange, and the next row under way, took the latter from 16.7.
 #include "layers.h"
 
