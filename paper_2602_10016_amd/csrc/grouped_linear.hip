@@ -147,12 +147,12 @@ __global__ __launch_bounds__(64 * DEEP_WAVES, 2) void grouped_rows_deep_kernel(c
     char* const mine = lds + wave * (2 * S::STAGE);
     if (t.group < G) {
         const T* wg = w + (int64_t)t.group * K * N;
-        GroupedDma<T, DEEP, 1, S::STEP_BYTES, false> dma_a;
-        GroupedDma<T, DEEP, 1, S::STEP_BYTES, B_COLUMNS> dma_b;
+        GroupedDma<T, DEEP, 1, false> dma_a;
+        GroupedDma<T, DEEP, 1, B_COLUMNS> dma_b;
         dma_a.init({(const char*)(in + t.row0 * K), (uint32_t)K * E, t.rows}, lane, 0);
         dma_b.init({(const char*)(B_COLUMNS ? wg + n0 : wg + (int64_t)n0 * K), (uint32_t)(B_COLUMNS ? N : K) * E, N - n0}, lane, 0);
-        GroupedFrag<T, DEEP, S::STEP_BYTES, false> frag_a;
-        GroupedFrag<T, DEEP, S::STEP_BYTES, B_COLUMNS> frag_b;
+        GroupedFrag<T, DEEP, false> frag_a;
+        GroupedFrag<T, DEEP, B_COLUMNS> frag_b;
         frag_a.init(lane, 0);
         frag_b.init(lane, 0);
         constexpr int STEP = decltype(dma_a)::STEP, LOADS = decltype(dma_a)::LOADS + decltype(dma_b)::LOADS;

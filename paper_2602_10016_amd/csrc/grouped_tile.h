@@ -2,15 +2,19 @@
 //
 // An operand lies in memory with the contraction along its rows ("row form": [rows, contraction]) or across them ("column form":
 // [contraction, columns]).  y = x w has A in row form and B in column form, dx = dy w^T both in row form, dw = x^T dy both in column
-// form; nothing is transposed in memory.  Steps of 64 contraction values travel straight from memory into a ring of LDS stages
-// (buffer loads to LDS); fragments of a row-form tile are 16-byte reads, of a column-form tile transposing reads (mfma_tile.h).
+// form; nothing is transposed in memory.  Steps of 128 bytes of contraction values (64 bf16, 32 fp32) travel straight from memory into a
+// ring of LDS stages (buffer loads to LDS); fragments of a row-form tile are 16-byte reads, of a column-form tile transposing reads
+// (bf16, mfma_tile.h) or four reads of a value (fp32).
 //   LDS, row form:     128 bytes per row, 16-byte chunk ^= (row / 2) % 8: 16 consecutive rows of one chunk hit 16 different places
-//   LDS, column form:  2 W bytes per contraction row, 64-byte group ^= row % 4 (W = 64: (row / 2) % 2, W = 32: nothing): four rows of one group, likewise
+//   LDS, column form:  W values per contraction row; bf16: 64-byte group ^= row % 4 (W = 64: (row / 2) % 2, W = 32: nothing), so that four
+//                      rows of one group do, too
+// fp32 takes v_mfma_f32_32x32x2_f32, whose two contraction values come from the two lane halves: with 16-byte fragments, value t of the chunks
+// 2c and 2c + 1.  The order of the contraction is the same for both operands, so it need not be the memory's.
 // What lies outside is handled where it is loaded: rows and columns of C outside the tile re-read the last valid one (never stored);
 // contraction values outside are zeros in both operands (a buffer load outside its descriptor's range gives zero), so that an infinity next
 // to them does no harm.
 // The matrix instructions compute C^T = B^T A^T, so that a lane holds consecutive columns of one row of C, which go out through LDS as
-// whole rows.
+// whole rows, with streaming stores: 139 264 rows, 256 -> 768, 95 -> 85 us, 768 -> 256, 84 -> 76.
 #pragma once
 #include "lds_ring.h"
 
@@ -19,7 +23,8 @@ namespace kunlun {
 // s_waitcnt that waits for LDS operations only.
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4)); }
 
-constexpr uint32_t GL_OUTSIDE = 0x80000000u;     // an offset outside every descriptor
+constexpr int GL_STEP_BYTES = 128;            // of contraction values per step
+constexpr uint32_t GL_OUTSIDE = 0x80000000u;  // an offset outside every descriptor
 
 // What a workgroup reads: `base` is the tile's first row (row form) or its first column in the first contraction row (column form).
 struct GroupedOperand {
@@ -29,12 +34,12 @@ struct GroupedOperand {
 };
 
 // DMA of one operand tile: EXTENT rows or columns of C, one step of contraction values.
-template <typename T, int EXTENT, int WAVES, int STEP_BYTES, bool COLUMNS>
+template <typename T, int EXTENT, int WAVES, bool COLUMNS>
 struct GroupedDma {
-    static constexpr int E = sizeof(T), STEP = STEP_BYTES / E, BYTES = EXTENT * STEP_BYTES;
+    static constexpr int E = sizeof(T), STEP = GL_STEP_BYTES / E, BYTES = EXTENT * GL_STEP_BYTES;
     static constexpr int LOADS = BYTES / 1024 / WAVES;  // load instructions per wave and step
     static_assert(LOADS >= 1 && LOADS * 1024 * WAVES == BYTES, "a tile splits evenly over the waves");
-    static constexpr int ROW_BYTES = COLUMNS ? EXTENT * E : STEP_BYTES, CHUNKS = ROW_BYTES / 16, ROWS = 1024 / ROW_BYTES;
+    static constexpr int ROW_BYTES = COLUMNS ? EXTENT * E : GL_STEP_BYTES, CHUNKS = ROW_BYTES / 16, ROWS = 1024 / ROW_BYTES;
     static_assert(ROW_BYTES <= 1024, "a load instruction fills whole rows");
     uint32_t voff[LOADS];
     const char* base;
@@ -42,7 +47,7 @@ struct GroupedDma {
     int lane_, wave_;
 
     __device__ static __forceinline__ int swizzle(int row) {
-        if (!COLUMNS) return STEP_BYTES == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+        if (!COLUMNS) return (row >> 1) & 7;
         return E == 4 || ROW_BYTES == 64 ? 0 : ROW_BYTES >= 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
     }
     __device__ __forceinline__ int row_of(int i) const { return (wave_ * LOADS + i) * ROWS + lane_ / CHUNKS; }
@@ -65,7 +70,7 @@ struct GroupedDma {
     // Step k: contraction values STEP k .. of which `left` exist.
     __device__ __forceinline__ void issue(int64_t k, int left, uint32_t lds) const {
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + wave_ * (LOADS * 1024));
-        const char* const from = base + (COLUMNS ? k * STEP * ld : k * STEP_BYTES);
+        const char* const from = base + (COLUMNS ? k * STEP * ld : k * GL_STEP_BYTES);
         const uint32_t bytes = COLUMNS ? (uint32_t)(left < STEP ? left : STEP) * ld : span;
         u32x4 rsrc = make_rsrc_words(from, bytes);
 #pragma unroll
@@ -84,10 +89,10 @@ struct GroupedDma {
 // lane.
 template <typename T> struct GroupedFragOf { typedef bf16x8 type; };
 template <> struct GroupedFragOf<float> { typedef f32x4 type; };
-template <typename T, int EXTENT, int STEP_BYTES, bool COLUMNS>
+template <typename T, int EXTENT, bool COLUMNS>
 struct GroupedFrag {
     typedef typename GroupedFragOf<T>::type Frag;
-    static constexpr int E = sizeof(T), ROW_BYTES = COLUMNS ? EXTENT * E : STEP_BYTES;
+    static constexpr int E = sizeof(T), ROW_BYTES = COLUMNS ? EXTENT * E : GL_STEP_BYTES;
     int at[2];
     __device__ __forceinline__ void init(int lane, int first) {
         const int g = lane >> 5;
@@ -103,7 +108,7 @@ struct GroupedFrag {
             at[0] = 4 * g * ROW_BYTES + (first + (lane & 31)) * 4;
         } else {
             const int row = first + (lane & 31);
-            at[0] = row * ROW_BYTES + ((g ^ (STEP_BYTES == 128 ? (row >> 1) & 7 : (row >> 2) & 3)) << 4);
+            at[0] = row * ROW_BYTES + ((g ^ ((row >> 1) & 7)) << 4);
         }
     }
     // Chunk 2 c + g of the step's contraction values, of the lane's row (column) in block b of 32
@@ -129,12 +134,12 @@ __device__ __forceinline__ f32x16 grouped_mfma(f32x4 a, f32x4 b, f32x16 c) {
     return c;
 }
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int STEP_BYTES_ = 128>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct GroupedShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, STEP_BYTES = STEP_BYTES_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int WAVES = WM * WN, THREADS = WAVES * 64, PER_CU = 8 / WAVES;  // two waves per SIMD
     static constexpr int MB = BM / WM / 32, NB = BN / WN / 32;  // 32 x 32 blocks of a wave
-    static constexpr int A_BYTES = BM * STEP_BYTES, STAGE = A_BYTES + BN * STEP_BYTES;
+    static constexpr int A_BYTES = BM * GL_STEP_BYTES, STAGE = A_BYTES + BN * GL_STEP_BYTES;
     static constexpr int OUT_ROW = NB * 32 * 4 + 16, OUT = WAVES * 32 * OUT_ROW;  // 32 rows of a wave at a time, padded, room for fp32
     static constexpr int LDS = STAGES * STAGE > OUT ? STAGES * STAGE : OUT;
 };
@@ -143,7 +148,7 @@ struct GroupedShape {
 template <typename S, typename T, typename FragA, typename FragB>
 __device__ __forceinline__ void grouped_step(f32x16 (&acc)[S::NB][S::MB], const char* ta, const char* tb, const FragA& frag_a, const FragB& frag_b) {
 #pragma unroll
-    for (int c = 0; c < S::STEP_BYTES / 32; ++c) {
+    for (int c = 0; c < GL_STEP_BYTES / 32; ++c) {
         typename GroupedFragOf<T>::type fa[S::MB], fb[S::NB];
 #pragma unroll
         for (int mb = 0; mb < S::MB; ++mb) fa[mb] = frag_a.read(ta, mb, c);
@@ -160,12 +165,12 @@ __device__ __forceinline__ void grouped_step(f32x16 (&acc)[S::NB][S::MB], const 
 template <typename S, typename T, bool A_COLUMNS, bool B_COLUMNS>
 __device__ __forceinline__ void grouped_product(f32x16 (&acc)[S::NB][S::MB], char* lds, const GroupedOperand& a, const GroupedOperand& b, int length,
                                                 int lane, int wave) {
-    GroupedDma<T, S::BM, S::WAVES, S::STEP_BYTES, A_COLUMNS> dma_a;
-    GroupedDma<T, S::BN, S::WAVES, S::STEP_BYTES, B_COLUMNS> dma_b;
+    GroupedDma<T, S::BM, S::WAVES, A_COLUMNS> dma_a;
+    GroupedDma<T, S::BN, S::WAVES, B_COLUMNS> dma_b;
     dma_a.init(a, lane, wave);
     dma_b.init(b, lane, wave);
-    GroupedFrag<T, S::BM, S::STEP_BYTES, A_COLUMNS> frag_a;
-    GroupedFrag<T, S::BN, S::STEP_BYTES, B_COLUMNS> frag_b;
+    GroupedFrag<T, S::BM, A_COLUMNS> frag_a;
+    GroupedFrag<T, S::BN, B_COLUMNS> frag_b;
     const int row0 = wave / S::WN * (S::BM / S::WM), col0 = wave % S::WN * (S::BN / S::WN);
     frag_a.init(lane, row0);
     frag_b.init(lane, col0);

@@ -213,3 +213,20 @@ def test_wrong_offsets_are_found_where_they_are_looked_for(kb):
                 kb.grouped_linear_bwd(x, w, x[:, :8].contiguous(), bad)
     finally:
         kb.verify_offsets(False)
+
+
+def test_two_streams_at_once(kb):
+    """Calls of two streams with workspaces of their own do not touch each other."""
+    big = lambda seed: dict(problem(torch.bfloat16, seed), ids=torch.randint(-1, V, (96,), device="cuda", generator=torch.Generator("cuda").manual_seed(seed)))
+    a, b = big(8), big(9)
+    want = parts(kb, a), parts(kb, b)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [[], []]
+    for _ in range(20):
+        for k, (s, p) in enumerate(zip(streams, (a, b))):
+            with torch.cuda.stream(s):
+                got[k].append(parts(kb, p))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(x, y) for run in got[k] for x, y in zip(run, want[k]))
